@@ -64,6 +64,8 @@ typedef enum gsd_status {
 
 #define GSD_DEV_BOUNDS       0x400u /* checking build (libgsd_check.so) only: a kernel formed an index outside its tensor; the access was skipped */
 
+#define GSD_DEV_BAD_KV       0x800u /* gsd_commit_kv_q8, gsd_append_kv_q8: a row held an infinity (stored as the largest code) or a NaN (stored as zero) */
+
 #define GSD_MAX_NODES 512          /* largest supported N (draft nodes per sequence) */
 
 /* kernel selection for gsd_verify_attn */
@@ -419,6 +421,131 @@ typedef struct gsd_commit_params {
 int gsd_commit_kv(void* k_cache, void* v_cache, const void* draft_k, const void* draft_v,
                   const int32_t* accepted_nodes, const int32_t* accepted_len, int32_t* seq_lens,
                   const gsd_commit_params* p, int32_t* status, void* stream);
+
+/*
+ * The 8-bit KV cache.  The paper keeps the committed prefix in a KV cache (Sec. 4.2) and does not say how it is
+ * stored; held in 8 bits it takes half of the memory, and of the time that attention spends on reading it.
+ *
+ *   codes      [B, Lmax, Hkv, D] bytes, K and V each: e4m3 (GSD_KV8_E4M3) or two's complement (GSD_KV8_INT8)
+ *   exponents  [B, ceil(Lmax / block), Hkv] int8, K and V each: rows j of block j / block of a head share a scale
+ *   value      code * 2^exponent, which bf16 and fp32 hold exactly
+ *
+ * `block` is 16, 32, 64 or 128 tokens.  What gsd_commit_kv_q8 and gsd_append_kv_q8 write has exponents from
+ * GSD_KV8_EXP_MIN to GSD_KV8_EXP_MAX, codes from -127 to 127 (int8) and no NaN (e4m3).  Codes and exponents of
+ * rows at positions >= seq_lens[b] may be anything.
+ */
+#define GSD_KV8_E4M3 0
+#define GSD_KV8_INT8 1
+#define GSD_KV8_EXP_MIN (-117)
+#define GSD_KV8_EXP_MAX 119
+typedef struct gsd_kv8_params {
+    int32_t format;   /* GSD_KV8_E4M3 or GSD_KV8_INT8 */
+    int32_t block;    /* tokens of a scale block: 16, 32, 64 or 128 */
+} gsd_kv8_params;
+
+/*
+ * gsd_verify_attn_q8 - gsd_verify_attn over an 8-bit cache (tree attention, Sec. 4.1; KV cache, Sec. 4.2).
+ *
+ * For every sequence b, node n and query head h (kv head c = h / (Hq/Hkv)):
+ *   K_j = k_cache[b,j,c,:] * 2^k_exp[b, j / block, c], V_j likewise, for cache rows j < seq_lens[b];
+ *   K_j, V_j = draft_k, draft_v[b,j,c,:] for draft rows j with bit j of ancestor_mask[b][n] set
+ *   out[b,n,h,:] = sum_j softmax_j(scale * <q[b,n,h,:], K_j>) * V_j
+ * The codes are used as they stand; on the way to the products only the softmax weights are rounded, to bf16 or finer (a
+ * weight times its V scale that is below 2^-28 of the largest such product of the row: to 2^-39 of that).  Sums and
+ * statistics are fp32, the output is bf16.  With N = 1 and a mask of one set bit it is ordinary
+ * single-token decoding.  Everything else is as for gsd_verify_attn: literal mask bits, rows at positions >=
+ * seq_lens[b] never reach the result whatever their codes and exponents are, a row with no visible key yields zeros.
+ * Exponents below -117 or above 119 and e4m3's NaN codes are not expected in visible rows.
+ *
+ *   q, draft_k, draft_v, ancestor_mask, seq_lens, out, workspace, status, stream   as for gsd_verify_attn
+ *   k_cache, v_cache  [B, Lmax, Hkv, D] codes  device  in, 16-byte aligned
+ *   k_exp, v_exp      [B, ceil(Lmax / block), Hkv] int8  device  in
+ *   p                 host; num_splits is 0 (choose) or the number of key ranges; GSD_ATTN_SPLIT_BALANCED and
+ *                     GSD_ATTN_SPLIT_PER_SEQUENCE are read as 0.  kernel: GSD_ATTN_AUTO, GSD_ATTN_MMA, or
+ *                     GSD_ATTN_TCGEN05 (as for gsd_verify_attn, D == 128 and a group size that divides 128)
+ *   c                 host
+ *   workspace         gsd_verify_attn_q8_workspace_bytes(p, c) bytes, 256-byte aligned
+ */
+size_t gsd_verify_attn_q8_workspace_bytes(const gsd_attn_params* p, const gsd_kv8_params* c);
+int gsd_verify_attn_q8(const void* q, const void* k_cache, const void* v_cache, const int8_t* k_exp, const int8_t* v_exp,
+                       const void* draft_k, const void* draft_v, const uint32_t* ancestor_mask, const int32_t* seq_lens,
+                       void* out, const gsd_attn_params* p, const gsd_kv8_params* c, void* workspace,
+                       size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * gsd_commit_kv_q8 - gsd_commit_kv into an 8-bit cache: the draft K/V rows of the accepted path are rounded and
+ * stored behind position seq_lens[b], and seq_lens[b] is advanced (cache update, Sec. 7.1 / Table 3).
+ *
+ * For each block of rows and each kv head that gets new rows x:
+ *   e(x)     = the least e in [GSD_KV8_EXP_MIN, GSD_KV8_EXP_MAX] with max|x| <= QMAX * 2^e (the upper end if there is
+ *              none); QMAX = 448 for e4m3, 127 for int8
+ *   exponent = max(its present exponent, e(x)) if the block holds rows before seq_lens[b], else e(x)
+ *   codes    = x * 2^-exponent rounded to the nearest code, ties to even, saturating; if the exponent has grown, the
+ *              codes of the block's earlier rows are rounded likewise to the new scale
+ * A NaN is stored as zero and an infinity as the largest code (GSD_DEV_BAD_KV).  Everything else is as for
+ * gsd_commit_kv; D is 64 or 128, B at most 65535.
+ */
+int gsd_commit_kv_q8(void* k_cache, void* v_cache, int8_t* k_exp, int8_t* v_exp, const void* draft_k, const void* draft_v,
+                     const int32_t* accepted_nodes, const int32_t* accepted_len, int32_t* seq_lens,
+                     const gsd_commit_params* p, const gsd_kv8_params* c, int32_t* status, void* stream);
+
+typedef struct gsd_append_params {
+    int32_t B;     /* sequences, at most 65535 */
+    int32_t T;     /* rows per sequence in k / v */
+    int32_t Hkv;   /* key/value heads */
+    int32_t D;     /* head dimension: 64 or 128 */
+    int32_t Lmax;  /* rows per sequence in k_cache / v_cache */
+} gsd_append_params;
+
+/*
+ * gsd_append_kv_q8 - the rows of a prompt, or of the next chunk of one, into an 8-bit cache: k[b][0..counts[b]) and
+ * v[b][0..counts[b]) are rounded and stored behind position seq_lens[b], by the rules of gsd_commit_kv_q8, and seq_lens[b]
+ * is advanced.  Rows that would land at or past Lmax are dropped (GSD_DEV_CACHE_FULL); a count outside [0, T] is clamped
+ * (GSD_DEV_BAD_SEQ_LEN).
+ *
+ *   k_cache, v_cache, k_exp, v_exp   device in/out
+ *   k, v      [B, T, Hkv, D] bf16 device in;  counts [B] int32 device in;  seq_lens [B] int32 device in/out
+ * Tensor bases 16-byte aligned.  No workspace, no allocation, asynchronous on `stream`.
+ */
+int gsd_append_kv_q8(void* k_cache, void* v_cache, int8_t* k_exp, int8_t* v_exp, const void* k, const void* v,
+                     const int32_t* counts, int32_t* seq_lens, const gsd_append_params* p, const gsd_kv8_params* c,
+                     int32_t* status, void* stream);
+
+/*
+ * gsd_token_logprobs - what a server returns beside the tokens that a step emitted: the log probability of each under
+ * the target model (the p of the acceptance rule, Sec. 3), the entropy of the distribution it came from, and the
+ * best alternatives.
+ *
+ * For every sequence b and i < lens[b], with the row x = logits[b][nodes[b][i]] and t = tokens[b][i]:
+ *   logprobs[b,i]        = x_t - lse(x),  lse(x) = log sum_j exp(x_j)
+ *   entropy[b,i]         = lse(x) - sum_j p_j x_j,  p_j = exp(x_j - lse(x)); entries at -inf add nothing
+ *   top_tokens[b,i,:]    = the k largest entries of x, best first, ties to the lowest index
+ *   top_logprobs[b,i,:]  = their log probabilities
+ * accepted_nodes, accepted_tokens and accepted_len of the acceptance calls can be passed as they are: the token at
+ * place i was emitted from the logits row of the node at place i.  Entries i >= lens[b] are set to 0 (tokens: -1).  A token
+ * outside [0, V) has the log probability NaN (GSD_DEV_BAD_TOKEN); a node outside [0, N) and a row without a finite
+ * entry, or with +inf or NaN (GSD_DEV_BAD_LOGITS), have NaN everywhere and tokens -1.
+ *
+ *   logits        [B, N, V] fp32 device in, 4-byte aligned
+ *   nodes         [B, T] int32 device in;  tokens [B, T] int32 device in;  lens [B] int32 device in (clamped to [0, T])
+ *   logprobs      [B, T] fp32 device out
+ *   entropy       [B, T] fp32 device out or NULL
+ *   top_tokens    [B, T, k] int32 device out, top_logprobs [B, T, k] fp32 device out; both may be NULL if k is 0
+ *   p             host; 0 <= k <= min(GSD_LOGPROBS_MAX_K, V)
+ *   workspace     device scratch of gsd_token_logprobs_workspace_bytes(p) bytes, 8-byte aligned, arbitrary contents
+ *   status        device int32 word or NULL (GSD_DEV_BAD_TOKEN, GSD_DEV_BAD_CSR for a node out of range, GSD_DEV_BAD_LOGITS)
+ * The sums are fp32 (ex2.approx).  Asynchronous on `stream`, allocates nothing.
+ */
+#define GSD_LOGPROBS_MAX_K 32
+typedef struct gsd_logprobs_params {
+    int32_t B, N, V;
+    int32_t T;     /* row length of nodes / tokens, 1..GSD_MAX_NODES */
+    int32_t k;     /* alternatives per token */
+} gsd_logprobs_params;
+size_t gsd_token_logprobs_workspace_bytes(const gsd_logprobs_params* p);
+int gsd_token_logprobs(const float* logits, const int32_t* nodes, const int32_t* tokens, const int32_t* lens, float* logprobs,
+                       float* entropy, int32_t* top_tokens, float* top_logprobs, const gsd_logprobs_params* p,
+                       void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
 
 /*
  * gsd_verify_step_host - one whole verification step from HOST buffers: copies every

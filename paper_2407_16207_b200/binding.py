@@ -55,12 +55,27 @@ class DraftParams(ctypes.Structure):
                 ("theta_prob", ctypes.c_float), ("theta_sib", ctypes.c_float)]
 
 
+class Kv8Params(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
+class AppendParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("Lmax", ctypes.c_int32)]
+
+
+class LogprobsParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("V", ctypes.c_int32), ("T", ctypes.c_int32),
+                ("k", ctypes.c_int32)]
+
+
 EXPORTS = ["gsd_version", "gsd_status_string", "gsd_last_cuda_error", "gsd_debug_attn_wait", "gsd_verify_attn",
            "gsd_verify_attn_workspace_bytes", "gsd_verify_attn_num_splits", "gsd_accept",
            "gsd_accept_workspace_bytes", "gsd_accept_static", "gsd_accept_sampled",
            "gsd_accept_sampled_workspace_bytes", "gsd_draft_expand", "gsd_draft_expand_workspace_bytes",
            "gsd_commit_kv", "gsd_build_mask", "gsd_unmerge_tree", "gsd_verify_step_host",
-           "gsd_verify_step_host_arena_bytes"]
+           "gsd_verify_step_host_arena_bytes", "gsd_verify_attn_q8", "gsd_verify_attn_q8_workspace_bytes",
+           "gsd_commit_kv_q8", "gsd_append_kv_q8", "gsd_token_logprobs", "gsd_token_logprobs_workspace_bytes"]
 
 
 def library_path() -> str:
@@ -114,6 +129,19 @@ def lib() -> ctypes.CDLL:
         L.gsd_verify_step_host_arena_bytes.restype = sz
         L.gsd_verify_step_host_arena_bytes.argtypes = [ctypes.POINTER(AttnParams),
                                                        ctypes.POINTER(AcceptParams)]
+        kv8 = ctypes.POINTER(Kv8Params)
+        L.gsd_verify_attn_q8.restype = i32
+        L.gsd_verify_attn_q8.argtypes = [vp] * 10 + [ctypes.POINTER(AttnParams), kv8, vp, sz, vp, vp]
+        L.gsd_verify_attn_q8_workspace_bytes.restype = sz
+        L.gsd_verify_attn_q8_workspace_bytes.argtypes = [ctypes.POINTER(AttnParams), kv8]
+        L.gsd_commit_kv_q8.restype = i32
+        L.gsd_commit_kv_q8.argtypes = [vp] * 9 + [ctypes.POINTER(CommitParams), kv8, vp, vp]
+        L.gsd_append_kv_q8.restype = i32
+        L.gsd_append_kv_q8.argtypes = [vp] * 8 + [ctypes.POINTER(AppendParams), kv8, vp, vp]
+        L.gsd_token_logprobs.restype = i32
+        L.gsd_token_logprobs.argtypes = [vp] * 8 + [ctypes.POINTER(LogprobsParams), vp, sz, vp, vp]
+        L.gsd_token_logprobs_workspace_bytes.restype = sz
+        L.gsd_token_logprobs_workspace_bytes.argtypes = [ctypes.POINTER(LogprobsParams)]
         _lib = L
     return _lib
 
@@ -121,7 +149,9 @@ def lib() -> ctypes.CDLL:
 # The library's functions the extension calls, in the order of its table.
 _NATIVE_CALLS = ("gsd_verify_attn", "gsd_verify_attn_workspace_bytes", "gsd_accept", "gsd_accept_workspace_bytes",
                  "gsd_accept_sampled", "gsd_accept_sampled_workspace_bytes", "gsd_binding_draft_expand",
-                 "gsd_draft_expand_workspace_bytes", "gsd_build_mask", "gsd_commit_kv")
+                 "gsd_draft_expand_workspace_bytes", "gsd_build_mask", "gsd_commit_kv", "gsd_verify_attn_q8",
+                 "gsd_verify_attn_q8_workspace_bytes", "gsd_commit_kv_q8", "gsd_append_kv_q8", "gsd_token_logprobs",
+                 "gsd_token_logprobs_workspace_bytes")
 _native = None
 _native_lib: Optional[ctypes.CDLL] = None      # the library the extension is bound to
 
@@ -512,6 +542,190 @@ def gsd_commit_kv(k_cache, v_cache, draft_k, draft_v, accepted_nodes, accepted_l
                                    draft_v.data_ptr(), accepted_nodes.data_ptr(),
                                    accepted_len.data_ptr(), seq_lens.data_ptr(), ctypes.byref(p),
                                    _ptr(status), _stream(k_cache)))
+
+
+GSD_KV8_E4M3, GSD_KV8_INT8 = 0, 1
+GSD_KV8_EXP_MIN, GSD_KV8_EXP_MAX = -117, 119
+_KV8_FORMATS = {torch.float8_e4m3fn: GSD_KV8_E4M3, torch.int8: GSD_KV8_INT8}
+
+
+def _check_kv8(k_cache, v_cache, k_exp, v_exp, block) -> Kv8Params:
+    """The 8-bit cache: codes [B,Lmax,Hkv,D] of float8_e4m3fn or int8, exponents [B,ceil(Lmax/block),Hkv] int8."""
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be [B,Lmax,Hkv,D]")
+    if k_cache.dtype not in _KV8_FORMATS:
+        raise ValueError(f"k_cache: expected torch.float8_e4m3fn or torch.int8, got {k_cache.dtype}")
+    if block not in (16, 32, 64, 128):
+        raise ValueError(f"block must be 16, 32, 64 or 128, got {block}")
+    B, Lmax, Hkv, D = k_cache.shape
+    _want(k_cache, k_cache.dtype, (B, Lmax, Hkv, D), "k_cache", True)
+    _want(v_cache, k_cache.dtype, (B, Lmax, Hkv, D), "v_cache", True)
+    nb = (Lmax + block - 1) // block
+    _want(k_exp, torch.int8, (B, nb, Hkv), "k_exp", True)
+    _want(v_exp, torch.int8, (B, nb, Hkv), "v_exp", True)
+    return Kv8Params(_KV8_FORMATS[k_cache.dtype], int(block))
+
+
+def gsd_verify_attn_q8_workspace_bytes(B, N, Hq, Hkv, D, Lmax, *, block, num_splits=0, kernel=GSD_ATTN_AUTO) -> int:
+    p = AttnParams(B, N, Hq, Hkv, D, Lmax, 0.0, num_splits, kernel)
+    c = Kv8Params(GSD_KV8_E4M3, block)
+    return int(lib().gsd_verify_attn_q8_workspace_bytes(ctypes.byref(p), ctypes.byref(c)))
+
+
+def gsd_verify_attn_q8(q, k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, ancestor_mask, seq_lens,
+                       out: Optional[torch.Tensor] = None, *, block: int, softmax_scale: float = 0.0,
+                       num_splits: int = 0, kernel: int = GSD_ATTN_AUTO,
+                       workspace: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """gsd_verify_attn over a cache held in 8 bits (codes float8_e4m3fn or int8, int8 exponents of a scale for each
+    `block` tokens and kv head); see gsd_verify_attn_q8 in include/gsd.h.  Enqueued on the current stream; returns
+    `out` [B,N,Hq,D] bf16."""
+    fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+    r = fast.verify_attn_q8(q, k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, ancestor_mask, seq_lens, out, block,
+                            softmax_scale, num_splits, kernel, workspace, status)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r)
+        return r
+    if q.dim() != 4:
+        raise ValueError("q must be [B,N,Hq,D]")
+    c = _check_kv8(k_cache, v_cache, k_exp, v_exp, block)
+    bf = torch.bfloat16
+    B, N, Hq, D = q.shape
+    Lmax, Hkv = k_cache.shape[1], k_cache.shape[2]
+    _want(q, bf, (B, N, Hq, D), "q", True)
+    _want(k_cache, k_cache.dtype, (B, Lmax, Hkv, D), "k_cache", True)
+    _want(draft_k, bf, (B, N, Hkv, D), "draft_k", True)
+    _want(draft_v, bf, (B, N, Hkv, D), "draft_v", True)
+    if ancestor_mask.dtype not in (torch.int32, torch.uint32):
+        raise ValueError("ancestor_mask must hold 32-bit words (int32 or uint32)")
+    _want(ancestor_mask, ancestor_mask.dtype, (B, N, (N + 31) // 32), "ancestor_mask", True)
+    _want(seq_lens, torch.int32, (B,), "seq_lens", True)
+    _same_device(q, k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, ancestor_mask, seq_lens, out, workspace, status)
+    if out is None:
+        out = torch.empty_like(q)
+    _want(out, bf, q.shape, "out", True)
+    p = _attn_params(q, k_cache, draft_k, softmax_scale, num_splits, kernel)
+    L = lib()
+    with torch.cuda.device(q.device):
+        need = int(L.gsd_verify_attn_q8_workspace_bytes(ctypes.byref(p), ctypes.byref(c)))
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        _check(L.gsd_verify_attn_q8(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+                                    draft_k.data_ptr(), draft_v.data_ptr(), ancestor_mask.data_ptr(), seq_lens.data_ptr(),
+                                    out.data_ptr(), ctypes.byref(p), ctypes.byref(c), _ptr(workspace), ws_bytes, _ptr(status),
+                                    _stream(q)))
+    return out
+
+
+def _same_device(first, *others) -> None:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError(f"tensors on {first.device} and {t.device}")
+
+
+def gsd_commit_kv_q8(k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, *,
+                     block: int, status: Optional[torch.Tensor] = None) -> None:
+    """Round the draft K/V rows of the accepted path into the 8-bit cache in place and advance seq_lens; see
+    gsd_commit_kv_q8 in include/gsd.h.  Enqueued on the current stream."""
+    fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+    r = fast.commit_kv_q8(k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, block, status)
+    if r is not None:
+        return _check(r)
+    c = _check_kv8(k_cache, v_cache, k_exp, v_exp, block)
+    B, Lmax, Hkv, D = k_cache.shape
+    if draft_k.dim() != 4 or accepted_nodes.dim() != 2:
+        raise ValueError("draft_k must be [B,N,Hkv,D] and accepted_nodes [B,Tcap]")
+    N, Tcap = draft_k.shape[1], accepted_nodes.shape[1]
+    _want(draft_k, torch.bfloat16, (B, N, Hkv, D), "draft_k", True)
+    _want(draft_v, torch.bfloat16, (B, N, Hkv, D), "draft_v", True)
+    _want(accepted_nodes, torch.int32, (B, Tcap), "accepted_nodes", True)
+    _want(accepted_len, torch.int32, (B,), "accepted_len", True)
+    _want(seq_lens, torch.int32, (B,), "seq_lens", True)
+    _same_device(k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, status)
+    p = CommitParams(B, N, Hkv, D, Lmax, Tcap)
+    with torch.cuda.device(k_cache.device):
+        _check(lib().gsd_commit_kv_q8(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+                                      draft_k.data_ptr(), draft_v.data_ptr(), accepted_nodes.data_ptr(),
+                                      accepted_len.data_ptr(), seq_lens.data_ptr(), ctypes.byref(p), ctypes.byref(c),
+                                      _ptr(status), _stream(k_cache)))
+
+
+def gsd_append_kv_q8(k_cache, v_cache, k_exp, v_exp, k, v, counts, seq_lens, *, block: int,
+                     status: Optional[torch.Tensor] = None) -> None:
+    """Round the first counts[b] rows of k / v [B,T,Hkv,D] into the 8-bit cache behind seq_lens[b] in place and advance
+    seq_lens; see gsd_append_kv_q8 in include/gsd.h.  Enqueued on the current stream."""
+    fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+    r = fast.append_kv_q8(k_cache, v_cache, k_exp, v_exp, k, v, counts, seq_lens, block, status)
+    if r is not None:
+        return _check(r)
+    c = _check_kv8(k_cache, v_cache, k_exp, v_exp, block)
+    B, Lmax, Hkv, D = k_cache.shape
+    if k.dim() != 4:
+        raise ValueError("k must be [B,T,Hkv,D]")
+    T = k.shape[1]
+    _want(k, torch.bfloat16, (B, T, Hkv, D), "k", True)
+    _want(v, torch.bfloat16, (B, T, Hkv, D), "v", True)
+    _want(counts, torch.int32, (B,), "counts", True)
+    _want(seq_lens, torch.int32, (B,), "seq_lens", True)
+    _same_device(k_cache, v_cache, k_exp, v_exp, k, v, counts, seq_lens, status)
+    p = AppendParams(B, T, Hkv, D, Lmax)
+    with torch.cuda.device(k_cache.device):
+        _check(lib().gsd_append_kv_q8(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
+                                      k.data_ptr(), v.data_ptr(), counts.data_ptr(), seq_lens.data_ptr(), ctypes.byref(p),
+                                      ctypes.byref(c), _ptr(status), _stream(k_cache)))
+
+
+def gsd_token_logprobs_workspace_bytes(B, N, V, T, k=0) -> int:
+    p = LogprobsParams(B, N, V, T, k)
+    return int(lib().gsd_token_logprobs_workspace_bytes(ctypes.byref(p)))
+
+
+def gsd_token_logprobs(logits, nodes, tokens, lens, *, k: int = 0, workspace: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None,
+                       out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]] = None
+                       ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Log probabilities of the tokens [B,T] under the logits rows of the nodes [B,T], entropy of these rows and their k
+    best entries; see gsd_token_logprobs in include/gsd.h.  Takes accepted_nodes, accepted_tokens, accepted_len of the
+    acceptance calls.  Returns (logprobs [B,T], entropy [B,T], top_tokens [B,T,k], top_logprobs [B,T,k])."""
+    if out is None:
+        fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+        r = fast.token_logprobs(logits, nodes, tokens, lens, k, workspace, status)
+        if r is not None:
+            if r.__class__ is int:
+                _check(r)
+            return r
+    if logits.dim() != 3 or nodes.dim() != 2:
+        raise ValueError("logits must be [B,N,V] and nodes [B,T]")
+    B, N, V = logits.shape
+    T = nodes.shape[1]
+    _want(logits, torch.float32, (B, N, V), "logits", True)
+    _want(nodes, torch.int32, (B, T), "nodes", True)
+    _want(tokens, torch.int32, (B, T), "tokens", True)
+    _want(lens, torch.int32, (B,), "lens", True)
+    dev = logits.device
+    if out is None:
+        n = max(int(k), 0)
+        out = (torch.empty((B, T), dtype=torch.float32, device=dev), torch.empty((B, T), dtype=torch.float32, device=dev),
+               torch.empty((B, T, n), dtype=torch.int32, device=dev), torch.empty((B, T, n), dtype=torch.float32, device=dev))
+    lp, ent, top, val = out
+    _want(lp, torch.float32, (B, T), "logprobs", True)
+    _want(ent, torch.float32, (B, T), "entropy", True)
+    _want(top, torch.int32, (B, T, max(int(k), 0)), "top_tokens", True)
+    _want(val, torch.float32, (B, T, max(int(k), 0)), "top_logprobs", True)
+    _same_device(logits, nodes, tokens, lens, lp, ent, top, val, workspace, status)
+    p = LogprobsParams(B, N, V, T, int(k))
+    L = lib()
+    with torch.cuda.device(dev):
+        need = int(L.gsd_token_logprobs_workspace_bytes(ctypes.byref(p)))
+        if workspace is None:
+            workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=dev)
+        _check(L.gsd_token_logprobs(logits.data_ptr(), nodes.data_ptr(), tokens.data_ptr(), lens.data_ptr(), lp.data_ptr(),
+                                    ent.data_ptr(), _ptr(top) if k else None, _ptr(val) if k else None, ctypes.byref(p),
+                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(status),
+                                    _stream(logits)))
+    return lp, ent, top, val
 
 
 GSD_STATIC_MAX_ROWS = 16384

@@ -244,6 +244,83 @@ extern "C" int gsd_verify_attn(const void* q, const void* k_cache, const void* v
     return rc;
 }
 
+// ---------------------------------------------------------------- the same over an 8-bit cache
+namespace {
+int attn_q8_params_ok(const gsd_attn_params* p, const gsd_kv8_params* c) {
+    const int ok = attn_params_ok(p);
+    if (ok != GSD_OK) return ok;
+    if (!c) return GSD_ERR_NULL_POINTER;
+    return kv8_block_log2(c) < 0 ? GSD_ERR_BAD_SHAPE : GSD_OK;
+}
+
+// Few stacked rows: items of 16 or 32 of them, key ranges for as many CTAs as the device holds.
+AttnPlan attn_q8_make_plan(const gsd_attn_params* p, int sm_count) {
+    AttnPlan pl = {};
+    const int R = p->N * (p->Hq / p->Hkv);
+    pl.kernel = GSD_ATTN_MMA;
+    pl.rows_per_item = attn_q8_mma_rows(R);
+    pl.part_rows = 64;
+    pl.dev.tiles_per_unit = (R + pl.rows_per_item - 1) / pl.rows_per_item;
+    pl.items = pl.dev.tiles_per_unit * p->B * p->Hkv;
+    pl.dev.items_a = pl.items;
+    pl.dev.splits_a = pl.dev.splits_b = 1;
+    const int resident = sm_count * attn_q8_mma_resident(R);
+    if (p->num_splits > 0) {
+        pl.dev.splits_a = p->num_splits;
+    } else if (pl.items < resident) {
+        const int tiles = (p->Lmax + 15) / 16 + (p->N + 15) / 16;
+        const int most = std::min(tiles / 16, 64);      // two tiles a warp at least
+        pl.dev.splits_a = std::max(1, std::min(resident / pl.items, most));
+    }
+    pl.ctas = pl.items * pl.dev.splits_a;
+    pl.slots = pl.dev.splits_a > 1 ? pl.ctas : 0;
+    pl.ws_bytes = pl.slots ? plan_part_o_bytes(pl, p->D) + plan_part_ml_bytes(pl) : 0;
+    return pl;
+}
+}  // namespace
+
+extern "C" size_t gsd_verify_attn_q8_workspace_bytes(const gsd_attn_params* p, const gsd_kv8_params* c) {
+    if (attn_q8_params_ok(p, c) != GSD_OK) return 0;
+    DeviceInfo di;
+    if (device_info(&di) != 0) return 0;
+    return attn_q8_make_plan(p, di.sm_count).ws_bytes;
+}
+
+extern "C" int gsd_verify_attn_q8(const void* q, const void* k_cache, const void* v_cache, const int8_t* k_exp,
+                                  const int8_t* v_exp, const void* draft_k, const void* draft_v,
+                                  const uint32_t* ancestor_mask, const int32_t* seq_lens, void* out,
+                                  const gsd_attn_params* p, const gsd_kv8_params* c, void* workspace,
+                                  size_t workspace_bytes, int32_t* status, void* stream) {
+    if (!p || !c || !q || !k_cache || !v_cache || !k_exp || !v_exp || !draft_k || !draft_v || !ancestor_mask || !seq_lens || !out)
+        return GSD_ERR_NULL_POINTER;
+    const int ok = attn_q8_params_ok(p, c);
+    if (ok != GSD_OK) return ok;
+    for (const void* ptr : {q, k_cache, v_cache, draft_k, draft_v, (const void*)out})
+        if (((uintptr_t)ptr & 15u) != 0) return GSD_ERR_MISALIGNED;
+    if (((uintptr_t)ancestor_mask & 3u) != 0 || ((uintptr_t)seq_lens & 3u) != 0) return GSD_ERR_MISALIGNED;
+    DeviceInfo di;
+    if (device_info(&di) != 0) return GSD_ERR_CUDA;
+    const AttnPlan plan = attn_q8_make_plan(p, di.sm_count);
+    if (plan.ws_bytes > 0) {
+        if (!workspace || workspace_bytes < plan.ws_bytes) return GSD_ERR_WORKSPACE;
+        if (((uintptr_t)workspace & 255u) != 0) return GSD_ERR_MISALIGNED;
+    }
+    AttnArgs a;
+    a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.draft_k = draft_k; a.draft_v = draft_v;
+    a.mask = ancestor_mask; a.seq_lens = seq_lens; a.out = out;
+    a.B = p->B; a.N = p->N; a.Hq = p->Hq; a.Hkv = p->Hkv; a.D = p->D; a.Lmax = p->Lmax;
+    a.G = p->Hq / p->Hkv; a.W = (p->N + 31) / 32;
+    const float scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->D);
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.plan = plan; a.workspace = workspace; a.status = status;
+    a.stream = (cudaStream_t)stream;
+    a.kv8.k_exp = k_exp; a.kv8.v_exp = v_exp; a.kv8.block_log2 = kv8_block_log2(c);
+    a.kv8.blocks = (p->Lmax + c->block - 1) / c->block; a.kv8.int8 = c->format == GSD_KV8_INT8;
+    int rc = launch_attn_q8_mma(a);
+    if (rc == GSD_OK && plan.slots > 0) rc = launch_attn_merge(a);
+    return rc;
+}
+
 // ---------------------------------------------------------------- host-buffer step
 namespace {
 struct ArenaLayout {

@@ -127,6 +127,18 @@ __host__ __device__ inline void plan_decode(const PlanDev& pl, int cta, int& ite
 AttnPlan attn_make_plan(const gsd_attn_params* p, int sm_count, bool by_length = true);
 
 // ---- verify-attention back ends (they validate nothing: the API layer did) ----
+// log2 of the tokens of a scale block, or -1 if the format or the block is not one of the cache's.
+inline int kv8_block_log2(const gsd_kv8_params* c) {
+    if (c->format != GSD_KV8_E4M3 && c->format != GSD_KV8_INT8) return -1;
+    for (int k = 4; k <= 7; ++k)
+        if (c->block == 1 << k) return k;
+    return -1;
+}
+struct Kv8Args {            // a cache held in 8 bits (gsd_verify_attn_q8)
+    const int8_t *k_exp, *v_exp;
+    int blocks, block_log2; // scale blocks of a sequence, log2 of the tokens of one
+    bool int8;              // codes: int8, else e4m3
+};
 struct AttnArgs {
     const void *q, *k_cache, *v_cache, *draft_k, *draft_v;
     const uint32_t* mask;
@@ -138,6 +150,7 @@ struct AttnArgs {
     void* workspace;
     int32_t* status;
     cudaStream_t stream;
+    Kv8Args kv8;
 };
 
 int attn_pick_kernel(const gsd_attn_params* p, int sm_count);   // GSD_ATTN_MMA or GSD_ATTN_TCGEN05
@@ -193,6 +206,9 @@ constexpr int kSeqPlanMaxSplit = 32;
 
 int launch_attn_plan(const AttnArgs& a);      // plans made on the device only: builds the table
 int launch_attn_mma(const AttnArgs& a);
+int launch_attn_q8_mma(const AttnArgs& a);
+int attn_q8_mma_rows(int R);                  // stacked rows of one of its items
+int attn_q8_mma_resident(int R);              // its CTAs an SM holds
 int launch_attn_tcgen05(const AttnArgs& a);
 bool attn_tcgen05_supports(int D, int G);
 int attn_tcgen05_rows(int G);                 // stacked rows of one row tile

@@ -1,0 +1,323 @@
+// gsd_commit_kv_q8 and gsd_append_kv_q8: bf16 K/V rows rounded into a cache held in 8 bits, behind the old end of every
+// sequence (the accepted path of a verification step, or the rows of a prompt).
+//
+// For every block of `block` tokens and kv head that gets new rows x:
+//   e(x)  = the least e with max |x| <= QMAX 2^e (QMAX 448 for e4m3, 127 for int8), within [-117, 119]
+//   e'    = max(e, e(x)) where the block holds earlier rows with exponent e, else e(x)
+//   codes = round(x 2^-e'), and of the earlier rows round(code 2^(e - e')), half to even, saturating
+// The scales are powers of two: the quotients are exact in fp32 (of a normal result), so a code is the correctly rounded one
+// on any machine, a row that is rounded again loses nothing to the quotient, and a reader may widen the codes and
+// apply the scale without a rounding of its own.
+//
+// An item is one block of one head of K or V; a group of 32 to 256 threads, as many as its rows need at eight
+// 16-byte pieces a thread, holds the item in registers: one read of the rows, the maximum by shuffles and shared memory, one
+// write.  Heads follow one another, so that groups side by side read whole rows.  Bound by DRAM for prompts, by two
+// dependent trips to memory (length and path, then the rows) for accepted paths; those go to one cluster of CTAs per
+// sequence, which may advance seq_lens itself once every CTA of it has read the old length.
+#include "gsd_internal.cuh"
+#include <initializer_list>
+
+namespace gsd {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPieces = 8;          // 16-byte pieces of a thread
+
+struct WriteArgs {
+    uint8_t *k_cache, *v_cache;
+    int8_t *k_exp, *v_exp;
+    const uint4 *k, *v;             // new rows [B, M, Hkv, D] bf16
+    const int32_t* nodes;           // [B, Tcap] rows to take, or nullptr: the first ones
+    const int32_t* count;
+    int32_t* seq_lens;
+    int32_t* status;
+    int M, Hkv, Lmax, Tcap, NB, block_log2;
+    int B;
+};
+
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ float two(int e) { return __int_as_float((e + 127) << 23); }     // 2^e, -126 <= e <= 127
+
+// Four values in units of the scale -> four codes.
+template <bool INT8>
+__device__ __forceinline__ uint32_t round4(float a, float b, float c, float d) {
+    if constexpr (INT8) {
+        auto r = [](float x) { return (uint32_t)__float2int_rn(fminf(fmaxf(x, -127.f), 127.f)) & 255u; };
+        return r(a) | r(b) << 8 | r(c) << 16 | r(d) << 24;
+    } else {
+        uint32_t w;
+        asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n mov.b32 %0, {l, h};\n}"
+            : "=r"(w) : "f"(a), "f"(b), "f"(c), "f"(d));
+        return w;
+    }
+}
+// Four codes in units of another scale.
+template <bool INT8>
+__device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
+    float x[4];
+    if constexpr (INT8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+    } else {
+        uint32_t p[2];
+        asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(p[0]), "=r"(p[1]) : "r"(w));
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(x[2 * i]), "=f"(x[2 * i + 1]) : "r"(p[i]));
+    }
+    return round4<INT8>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+}
+// The exponent that a largest magnitude (bf16 bits) asks for.
+template <bool INT8>
+__device__ __forceinline__ int least_exp(uint32_t top) {
+    const int e = INT8 ? (int)(top >> 7) - 133 + ((top & 127u) > 126u) : (int)(top >> 7) - 135 + ((top & 127u) > 96u);
+    return min(max(e, GSD_KV8_EXP_MIN), GSD_KV8_EXP_MAX);
+}
+
+// What a call appends to sequence b: `n` rows behind position L, those that fit.
+struct Span {
+    int L, n;
+};
+
+template <int D, bool INT8, bool CLUSTER>
+__global__ void __launch_bounds__(kThreads) kv8_write_kernel(WriteArgs a) {
+    constexpr int ROW_PIECES = D / 8;
+    __shared__ int s_src[GSD_MAX_NODES];
+    __shared__ int s_tot[kThreads / 32];
+    __shared__ uint32_t s_top[2][kThreads / 32];
+    let_successor_start();
+    const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    wait_for_predecessor();
+    Span s;
+    unsigned flags = 0;
+    s.L = a.seq_lens[b];
+    int want = a.count[b];
+    if (s.L < 0 || s.L > a.Lmax) {
+        flags |= GSD_DEV_BAD_SEQ_LEN;
+        s.L = s.L < 0 ? 0 : a.Lmax;
+    }
+    // (only now may another CTA of the cluster write the length)
+    if (CLUSTER) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (a.nodes) {
+        // the valid node ids of the path, in order: a ballot a warp, a scan over the warps
+        want = min(min(want, a.Tcap), GSD_MAX_NODES);
+        int base = 0;
+        for (int i0 = 0; i0 < want; i0 += kThreads) {
+            const int i = i0 + tid;
+            int node = -1;
+            if (i < want) {
+                node = a.nodes[(size_t)b * a.Tcap + i];
+                if (node < 0 || node >= a.M) { node = -1; flags |= GSD_DEV_BAD_CSR; }
+            }
+            const unsigned vote = __ballot_sync(0xFFFFFFFFu, node >= 0);
+            if (lane == 0) s_tot[warp] = __popc(vote);
+            __syncthreads();
+            int at = base;
+            for (int w = 0; w < kThreads / 32; ++w) {
+                if (w < warp) at += s_tot[w];
+                base += s_tot[w];
+            }
+            if (node >= 0) s_src[at + __popc(vote & ((1u << lane) - 1u))] = node;
+            __syncthreads();
+        }
+        want = base;
+    } else if (want < 0 || want > a.M) {
+        flags |= GSD_DEV_BAD_SEQ_LEN;
+        want = want < 0 ? 0 : a.M;
+    }
+    s.n = min(want, a.Lmax - s.L);
+    if (s.n < want) flags |= GSD_DEV_CACHE_FULL;
+
+    if (s.n > 0) {
+        const int block = 1 << a.block_log2, first = s.L >> a.block_log2, blocks = ((s.L + s.n - 1) >> a.block_log2) - first + 1;
+        const int pieces = min(block, s.n) * ROW_PIECES;                   // of an item, at most
+        int group = 32;
+        while (group < kThreads && group * kPieces < pieces) group <<= 1;
+        const int per_cta = kThreads / group, mine = tid / group, t = tid % group;
+        const int items = 2 * blocks * a.Hkv, step = (int)gridDim.x * per_cta;
+        int parity = 0;
+        for (int i0 = (int)blockIdx.x * per_cta; i0 < items; i0 += step, parity ^= 1) {
+            const int item = i0 + mine;
+            const bool in = item < items;
+            const int head = item % a.Hkv, blk = first + item / a.Hkv % blocks, is_v = item / a.Hkv / blocks;
+            const int lo = blk << a.block_log2;
+            const int r0 = max(lo, s.L), r1 = in ? min(lo + block, s.L + s.n) : r0;      // positions of the new rows
+            const uint4* src = (is_v ? a.v : a.k) + ((size_t)b * a.M * a.Hkv + head) * ROW_PIECES;
+            uint8_t* dst = (is_v ? a.v_cache : a.k_cache) + ((size_t)b * a.Lmax * a.Hkv + head) * D;
+            int8_t* ex = (is_v ? a.v_exp : a.k_exp) + ((size_t)b * a.NB + blk) * a.Hkv + head;
+            const bool held = in && lo < s.L;
+            const int e_old = held && GSD_IN_BOUNDS(blk < a.NB, a.status) ? *ex : GSD_KV8_EXP_MIN;
+            uint4 x[kPieces];
+            uint32_t top2 = 0;
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                const int at = k * group + t, pos = r0 + at / ROW_PIECES;
+                x[k] = make_uint4(0, 0, 0, 0);
+                if (pos < r1) {
+                    const int row = a.nodes ? s_src[pos - s.L] : pos - s.L;
+                    if (GSD_IN_BOUNDS(row >= 0 && row < a.M, a.status)) x[k] = src[(size_t)row * a.Hkv * ROW_PIECES + at % ROW_PIECES];
+                }
+            }
+            auto largest = [&]() {
+                top2 = 0;
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k)
+                    top2 = max_u16x2(top2, max_u16x2(max_u16x2(x[k].x & 0x7FFF7FFFu, x[k].y & 0x7FFF7FFFu), max_u16x2(x[k].z & 0x7FFF7FFFu, x[k].w & 0x7FFF7FFFu)));
+                return max(top2 & 0xFFFFu, top2 >> 16);
+            };
+            uint32_t top = largest();
+            if (top >= 0x7F80u) {
+                flags |= GSD_DEV_BAD_KV;
+                if (top > 0x7F80u) {                                       // a NaN is stored as zero
+                    auto clean = [](uint32_t& w) {
+                        if ((w & 0x7FFFu) > 0x7F80u) w &= 0xFFFF0000u;
+                        if ((w >> 16 & 0x7FFFu) > 0x7F80u) w &= 0xFFFFu;
+                    };
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k) { clean(x[k].x); clean(x[k].y); clean(x[k].z); clean(x[k].w); }
+                    top = largest();
+                }
+            }
+            top = __reduce_max_sync(0xFFFFFFFFu, top);
+            if (group > 32) {
+                // (two sets of words by turns: the next item's cannot overtake the reads of this one's)
+                if (lane == 0) s_top[parity][warp] = top;
+                __syncthreads();
+                const int w0 = mine * (group / 32);
+                for (int w = 0; w < group / 32; ++w) top = max(top, s_top[parity][w0 + w]);
+            }
+            if (!in) continue;
+            const int e = max(least_exp<INT8>(top), e_old);
+            const float f = two(-e);
+#pragma unroll
+            for (int k = 0; k < kPieces; ++k) {
+                const int at = k * group + t, pos = r0 + at / ROW_PIECES;
+                if (pos >= r1 || !GSD_IN_BOUNDS(pos >= 0 && pos < a.Lmax, a.status)) continue;
+                auto lo16 = [&](uint32_t w) { return __uint_as_float(w << 16) * f; };
+                auto hi16 = [&](uint32_t w) { return __uint_as_float(w & 0xFFFF0000u) * f; };
+                uint2 c;
+                c.x = round4<INT8>(lo16(x[k].x), hi16(x[k].x), lo16(x[k].y), hi16(x[k].y));
+                c.y = round4<INT8>(lo16(x[k].z), hi16(x[k].z), lo16(x[k].w), hi16(x[k].w));
+                *reinterpret_cast<uint2*>(dst + (size_t)pos * a.Hkv * D + at % ROW_PIECES * 8) = c;
+            }
+            if (held && e > e_old) {
+                // the earlier rows of the block in the new scale
+                const float g = e - e_old > 126 ? 0.f : two(e_old - e);
+                for (int at = t; at < (s.L - lo) * ROW_PIECES; at += group) {
+                    uint2* c = reinterpret_cast<uint2*>(dst + (size_t)(lo + at / ROW_PIECES) * a.Hkv * D + at % ROW_PIECES * 8);
+                    const uint2 w = *c;
+                    *c = make_uint2(rescale4<INT8>(w.x, g), rescale4<INT8>(w.y, g));
+                }
+            }
+            if (t == 0 && GSD_IN_BOUNDS(blk < a.NB, a.status)) *ex = (int8_t)e;
+        }
+    }
+    if (flags && a.status) atomicOr((unsigned*)a.status, flags);
+    if (CLUSTER) {
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (blockIdx.x == 0 && tid == 0) a.seq_lens[b] = s.L + s.n;
+    }
+}
+
+// The lengths behind a call whose CTAs are too many to meet.
+__global__ void __launch_bounds__(kThreads) kv8_advance_kernel(const int32_t* count, int32_t* seq_lens, int B, int M, int Lmax) {
+    let_successor_start();
+    wait_for_predecessor();
+    const int b = blockIdx.x * kThreads + threadIdx.x;
+    if (b >= B) return;
+    const int L = min(max(seq_lens[b], 0), Lmax);
+    seq_lens[b] = L + min(min(max(count[b], 0), M), Lmax - L);
+}
+
+constexpr int kCluster = 8;         // CTAs of a sequence that commits a path
+
+template <int D, bool INT8>
+int launch_write(const WriteArgs& a, cudaStream_t stream) {
+    DeviceInfo di;
+    if (device_info(&di) != 0) return GSD_ERR_CUDA;
+    if (a.nodes) {
+        // a warp's worth of rows an item, and at most two blocks for a path shorter than a block
+        const int items = 2 * a.Hkv * 2;
+        int ctas = 1;
+        while (ctas < kCluster && ctas * (kThreads / 32) < items) ctas <<= 1;
+        cudaLaunchAttribute attr[2];
+        dependent_launch_attr(attr);
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = ctas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(ctas, a.B);
+        cfg.blockDim = dim3(kThreads);
+        cfg.stream = stream;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        GSD_CUDA_TRY(cudaLaunchKernelEx(&cfg, kv8_write_kernel<D, INT8, true>, a));
+        return GSD_OK;
+    }
+    const int block = 1 << a.block_log2, pieces = (block < a.M ? block : a.M) * (D / 8);
+    int group = 32;
+    while (group < kThreads && group * kPieces < pieces) group <<= 1;
+    const int blocks = (a.M + block - 2) / block + 1;       // that M rows can touch
+    const long long items = 2ll * a.Hkv * blocks, per_cta = kThreads / group;
+    long long ctas = (items + per_cta - 1) / per_cta;
+    const long long most = ((long long)di.sm_count * 8 + a.B - 1) / a.B;
+    if (ctas > most) ctas = most;
+    GSD_CUDA_TRY(launch_dependent(kv8_write_kernel<D, INT8, false>, dim3((unsigned)ctas, a.B), dim3(kThreads), 0, stream, a));
+    GSD_CUDA_TRY(launch_dependent(kv8_advance_kernel, dim3((a.B + kThreads - 1) / kThreads), dim3(kThreads), 0, stream,
+                                  a.count, a.seq_lens, a.B, a.M, a.Lmax));
+    return GSD_OK;
+}
+
+int write_rows(WriteArgs& a, const gsd_kv8_params* c, int D, cudaStream_t stream) {
+    a.block_log2 = kv8_block_log2(c);
+    a.NB = (a.Lmax + c->block - 1) / c->block;
+    if (c->format == GSD_KV8_INT8) return D == 128 ? launch_write<128, true>(a, stream) : launch_write<64, true>(a, stream);
+    return D == 128 ? launch_write<128, false>(a, stream) : launch_write<64, false>(a, stream);
+}
+
+int misaligned(std::initializer_list<const void*> by16) {
+    for (const void* ptr : by16)
+        if (((uintptr_t)ptr & 15u) != 0) return 1;
+    return 0;
+}
+
+}  // namespace
+}  // namespace gsd
+
+extern "C" int gsd_commit_kv_q8(void* k_cache, void* v_cache, int8_t* k_exp, int8_t* v_exp, const void* draft_k, const void* draft_v,
+                                const int32_t* accepted_nodes, const int32_t* accepted_len, int32_t* seq_lens,
+                                const gsd_commit_params* p, const gsd_kv8_params* c, int32_t* status, void* stream) {
+    using namespace gsd;
+    if (!p || !c || !k_cache || !v_cache || !k_exp || !v_exp || !draft_k || !draft_v || !accepted_nodes || !accepted_len || !seq_lens)
+        return GSD_ERR_NULL_POINTER;
+    if (p->B < 1 || p->N < 1 || p->N > GSD_MAX_NODES || p->Hkv < 1 || (p->D != 64 && p->D != 128) || p->Lmax < 1 ||
+        p->Tcap < 1 || p->B > 65535 || p->Hkv > 65535 || kv8_block_log2(c) < 0)
+        return GSD_ERR_BAD_SHAPE;
+    if (misaligned({k_cache, v_cache, draft_k, draft_v})) return GSD_ERR_MISALIGNED;
+    WriteArgs a;
+    a.k_cache = (uint8_t*)k_cache; a.v_cache = (uint8_t*)v_cache; a.k_exp = k_exp; a.v_exp = v_exp;
+    a.k = (const uint4*)draft_k; a.v = (const uint4*)draft_v; a.nodes = accepted_nodes; a.count = accepted_len;
+    a.seq_lens = seq_lens; a.status = status;
+    a.B = p->B; a.M = p->N; a.Hkv = p->Hkv; a.Lmax = p->Lmax; a.Tcap = p->Tcap;
+    return write_rows(a, c, p->D, (cudaStream_t)stream);
+}
+
+extern "C" int gsd_append_kv_q8(void* k_cache, void* v_cache, int8_t* k_exp, int8_t* v_exp, const void* k, const void* v,
+                                const int32_t* counts, int32_t* seq_lens, const gsd_append_params* p, const gsd_kv8_params* c,
+                                int32_t* status, void* stream) {
+    using namespace gsd;
+    if (!p || !c || !k_cache || !v_cache || !k_exp || !v_exp || !k || !v || !counts || !seq_lens) return GSD_ERR_NULL_POINTER;
+    if (p->B < 1 || p->T < 1 || p->Hkv < 1 || (p->D != 64 && p->D != 128) || p->Lmax < 1 || p->B > 65535 || p->Hkv > 65535 ||
+        kv8_block_log2(c) < 0 || ((long long)p->T / c->block + 2) * 2 * p->Hkv > (1 << 30))
+        return GSD_ERR_BAD_SHAPE;
+    if (misaligned({k_cache, v_cache, k, v})) return GSD_ERR_MISALIGNED;
+    WriteArgs a;
+    a.k_cache = (uint8_t*)k_cache; a.v_cache = (uint8_t*)v_cache; a.k_exp = k_exp; a.v_exp = v_exp;
+    a.k = (const uint4*)k; a.v = (const uint4*)v; a.nodes = nullptr; a.count = counts;
+    a.seq_lens = seq_lens; a.status = status;
+    a.B = p->B; a.M = p->T; a.Hkv = p->Hkv; a.Lmax = p->Lmax; a.Tcap = 0;
+    return write_rows(a, c, p->D, (cudaStream_t)stream);
+}

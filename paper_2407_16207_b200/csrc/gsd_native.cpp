@@ -33,6 +33,12 @@ struct Table {
     decltype(&gsd_draft_expand_workspace_bytes) draft_expand_workspace_bytes;
     decltype(&gsd_build_mask) build_mask;
     decltype(&gsd_commit_kv) commit_kv;
+    decltype(&gsd_verify_attn_q8) verify_attn_q8;
+    decltype(&gsd_verify_attn_q8_workspace_bytes) verify_attn_q8_workspace_bytes;
+    decltype(&gsd_commit_kv_q8) commit_kv_q8;
+    decltype(&gsd_append_kv_q8) append_kv_q8;
+    decltype(&gsd_token_logprobs) token_logprobs;
+    decltype(&gsd_token_logprobs_workspace_bytes) token_logprobs_workspace_bytes;
 };
 constexpr Py_ssize_t kTable = sizeof(Table) / sizeof(void*);
 Table g;       // written under the GIL by bind(), copied under the GIL by every call
@@ -378,9 +384,158 @@ PyObject* py_commit_kv(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
     GSD_PY_END
 }
 
+// The 8-bit cache that argument `at` begins (k_cache, v_cache, k_exp, v_exp), with `block` tokens a scale block.
+struct Kv8 {
+    gsd_kv8_params c;
+    const at::Tensor *k, *v, *ke, *ve;
+    int32_t B, Lmax, Hkv, D;
+};
+bool kv8_args(Args& a, int at, int at_block, Kv8& s) {
+    const at::Tensor* k = plain(a.v[at]);
+    if (!k || k->dim() != 4 || (k->scalar_type() != at::kChar && k->scalar_type() != at::kFloat8_e4m3fn)) return a.ok = false;
+    s.k = a.tensor(at, k->scalar_type(), 4);
+    s.c.format = k->scalar_type() == at::kChar ? GSD_KV8_INT8 : GSD_KV8_E4M3;
+    s.c.block = a.i32(at_block);
+    s.B = a.size(k, 0); s.Lmax = a.size(k, 1); s.Hkv = a.size(k, 2); s.D = a.size(k, 3);
+    if (!a.ok || (s.c.block != 16 && s.c.block != 32 && s.c.block != 64 && s.c.block != 128)) return a.ok = false;
+    const int64_t blocks = ((int64_t)s.Lmax + s.c.block - 1) / s.c.block;
+    s.v = a.tensor(at + 1, k->scalar_type(), {s.B, s.Lmax, s.Hkv, s.D});
+    s.ke = a.tensor(at + 2, at::kChar, {s.B, blocks, s.Hkv});
+    s.ve = a.tensor(at + 3, at::kChar, {s.B, blocks, s.Hkv});
+    return a.ok;
+}
+
+// (q, k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, mask, seq_lens, out, block, scale, num_splits, kernel, workspace, status)
+PyObject* py_verify_attn_q8(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(16)
+    const at::Tensor* q = a.tensor(0, at::kBFloat16, 4);
+    Kv8 s;
+    if (!a.ok || !kv8_args(a, 1, 10, s)) Py_RETURN_NONE;
+    gsd_attn_params p;
+    p.B = a.size(q, 0); p.N = a.size(q, 1); p.Hq = a.size(q, 2); p.D = a.size(q, 3);
+    p.Lmax = s.Lmax; p.Hkv = s.Hkv;
+    GSD_PY_PLAIN;
+    if (s.B != p.B || s.D != p.D) Py_RETURN_NONE;
+    const at::Tensor* dk = a.tensor(5, at::kBFloat16, {p.B, p.N, p.Hkv, p.D});
+    const at::Tensor* dv = a.tensor(6, at::kBFloat16, {p.B, p.N, p.Hkv, p.D});
+    const at::Tensor* sl = a.tensor(8, at::kInt, {p.B});
+    GSD_PY_PLAIN;
+    const at::Tensor* mask = plain(argv[7]);
+    if (!mask || mask->get_device() != a.device || (mask->scalar_type() != at::kInt && mask->scalar_type() != at::kUInt32) ||
+        !mask->sizes().equals({p.B, p.N, ((int64_t)p.N + 31) / 32}))
+        Py_RETURN_NONE;
+    const at::Tensor* out = argv[9] == Py_None ? nullptr : a.tensor(9, at::kBFloat16, {p.B, p.N, p.Hq, p.D});
+    p.softmax_scale = a.f32(11); p.num_splits = a.i32(12); p.kernel = a.i32(13);
+    const at::Tensor* ws = a.any_or_none(14);
+    const at::Tensor* status = a.any_or_none(15);
+    GSD_PY_PLAIN;
+    Call c(a.device);
+    at::Tensor made;
+    if (!out) {
+        made = empty(q->sizes(), at::kBFloat16, a.device);
+        out = &made;
+    }
+    c.scratch(ws, ws ? 0 : lib.verify_attn_q8_workspace_bytes(&p, &s.c), a.device);
+    const int rc = unlocked([&] {
+        return lib.verify_attn_q8(ptr<void>(q), ptr<void>(s.k), ptr<void>(s.v), ptr<int8_t>(s.ke), ptr<int8_t>(s.ve), ptr<void>(dk),
+                                  ptr<void>(dv), ptr<uint32_t>(mask), ptr<int32_t>(sl), ptr<void>(out), &p, &s.c, c.ws, c.ws_bytes,
+                                  ptr<int32_t>(status), c.stream);
+    });
+    if (rc != GSD_OK) return PyLong_FromLong(rc);
+    if (!made.defined()) {
+        Py_INCREF(argv[9]);
+        return argv[9];
+    }
+    return THPVariable_Wrap(std::move(made));
+    GSD_PY_END
+}
+
+// (k_cache, v_cache, k_exp, v_exp, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, block, status); returns 0 when done
+PyObject* py_commit_kv_q8(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(11)
+    Kv8 s;
+    if (!kv8_args(a, 0, 9, s)) Py_RETURN_NONE;
+    const at::Tensor* dk = a.tensor(4, at::kBFloat16, 4);
+    const at::Tensor* nodes = a.tensor(6, at::kInt, 2);
+    GSD_PY_PLAIN;
+    gsd_commit_params p;
+    p.B = s.B; p.Lmax = s.Lmax; p.Hkv = s.Hkv; p.D = s.D;
+    p.N = a.size(dk, 1); p.Tcap = a.size(nodes, 1);
+    GSD_PY_PLAIN;
+    if (nodes->size(0) != p.B || !dk->sizes().equals({p.B, p.N, p.Hkv, p.D})) Py_RETURN_NONE;
+    const at::Tensor* dv = a.tensor(5, at::kBFloat16, {p.B, p.N, p.Hkv, p.D});
+    const at::Tensor* len = a.tensor(7, at::kInt, {p.B});
+    const at::Tensor* sl = a.tensor(8, at::kInt, {p.B});
+    const at::Tensor* status = a.any_or_none(10);
+    GSD_PY_PLAIN;
+    Call c(a.device);
+    return PyLong_FromLong(unlocked([&] {
+        return lib.commit_kv_q8(ptr<void>(s.k), ptr<void>(s.v), ptr<int8_t>(s.ke), ptr<int8_t>(s.ve), ptr<void>(dk), ptr<void>(dv),
+                                ptr<int32_t>(nodes), ptr<int32_t>(len), ptr<int32_t>(sl), &p, &s.c, ptr<int32_t>(status), c.stream);
+    }));
+    GSD_PY_END
+}
+
+// (k_cache, v_cache, k_exp, v_exp, k, v, counts, seq_lens, block, status); returns 0 when done
+PyObject* py_append_kv_q8(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(10)
+    Kv8 s;
+    if (!kv8_args(a, 0, 8, s)) Py_RETURN_NONE;
+    const at::Tensor* k = a.tensor(4, at::kBFloat16, 4);
+    GSD_PY_PLAIN;
+    gsd_append_params p;
+    p.B = s.B; p.Lmax = s.Lmax; p.Hkv = s.Hkv; p.D = s.D;
+    p.T = a.size(k, 1);
+    GSD_PY_PLAIN;
+    if (!k->sizes().equals({p.B, p.T, p.Hkv, p.D})) Py_RETURN_NONE;
+    const at::Tensor* v = a.tensor(5, at::kBFloat16, {p.B, p.T, p.Hkv, p.D});
+    const at::Tensor* counts = a.tensor(6, at::kInt, {p.B});
+    const at::Tensor* sl = a.tensor(7, at::kInt, {p.B});
+    const at::Tensor* status = a.any_or_none(9);
+    GSD_PY_PLAIN;
+    Call c(a.device);
+    return PyLong_FromLong(unlocked([&] {
+        return lib.append_kv_q8(ptr<void>(s.k), ptr<void>(s.v), ptr<int8_t>(s.ke), ptr<int8_t>(s.ve), ptr<void>(k), ptr<void>(v),
+                                ptr<int32_t>(counts), ptr<int32_t>(sl), &p, &s.c, ptr<int32_t>(status), c.stream);
+    }));
+    GSD_PY_END
+}
+
+// (logits, nodes, tokens, lens, k, workspace, status)
+PyObject* py_token_logprobs(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(7)
+    const at::Tensor* logits = a.tensor(0, at::kFloat, 3);
+    const at::Tensor* nodes = a.tensor(1, at::kInt, 2);
+    GSD_PY_PLAIN;
+    gsd_logprobs_params p;
+    p.B = a.size(logits, 0); p.N = a.size(logits, 1); p.V = a.size(logits, 2);
+    p.T = a.size(nodes, 1); p.k = a.i32(4);
+    GSD_PY_PLAIN;
+    if (nodes->size(0) != p.B || p.k < 0 || p.k > GSD_LOGPROBS_MAX_K) Py_RETURN_NONE;
+    const at::Tensor* tokens = a.tensor(2, at::kInt, {p.B, p.T});
+    const at::Tensor* lens = a.tensor(3, at::kInt, {p.B});
+    const at::Tensor* ws = a.any_or_none(5);
+    const at::Tensor* status = a.any_or_none(6);
+    GSD_PY_PLAIN;
+    Call c(a.device);
+    at::Tensor lp = empty({p.B, p.T}, at::kFloat, a.device), ent = empty({p.B, p.T}, at::kFloat, a.device);
+    at::Tensor top = empty({p.B, p.T, p.k}, at::kInt, a.device), val = empty({p.B, p.T, p.k}, at::kFloat, a.device);
+    c.scratch(ws, ws ? 0 : std::max<size_t>(lib.token_logprobs_workspace_bytes(&p), 8), a.device);
+    const int rc = unlocked([&] {
+        return lib.token_logprobs(ptr<float>(logits), ptr<int32_t>(nodes), ptr<int32_t>(tokens), ptr<int32_t>(lens), ptr<float>(&lp),
+                                  ptr<float>(&ent), p.k ? ptr<int32_t>(&top) : nullptr, p.k ? ptr<float>(&val) : nullptr, &p, c.ws,
+                                  c.ws_bytes, ptr<int32_t>(status), c.stream);
+    });
+    return rc != GSD_OK ? PyLong_FromLong(rc)
+                        : tuple_of({THPVariable_Wrap(lp), THPVariable_Wrap(ent), THPVariable_Wrap(top), THPVariable_Wrap(val)});
+    GSD_PY_END
+}
+
 #define GSD_PY_FN(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {GSD_PY_FN(bind), GSD_PY_FN(verify_attn), GSD_PY_FN(accept), GSD_PY_FN(accept_sampled),
-                         GSD_PY_FN(draft_expand), GSD_PY_FN(build_mask), GSD_PY_FN(commit_kv), {nullptr, nullptr, 0, nullptr}};
+                         GSD_PY_FN(draft_expand), GSD_PY_FN(build_mask), GSD_PY_FN(commit_kv),
+                         GSD_PY_FN(verify_attn_q8), GSD_PY_FN(commit_kv_q8), GSD_PY_FN(append_kv_q8),
+                         GSD_PY_FN(token_logprobs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
