@@ -450,12 +450,12 @@ typedef struct gsd_kv8_params {
  *   K_j = k_cache[b,j,c,:] * 2^k_exp[b, j / block, c], V_j likewise, for cache rows j < seq_lens[b];
  *   K_j, V_j = draft_k, draft_v[b,j,c,:] for draft rows j with bit j of ancestor_mask[b][n] set
  *   out[b,n,h,:] = sum_j softmax_j(scale * <q[b,n,h,:], K_j>) * V_j
- * The codes are used as they stand; on the way to the products only the softmax weights are rounded, to bf16 or finer (a
- * weight times its V scale that is below 2^-28 of the largest such product of the row: to 2^-39 of that).  Sums and
- * statistics are fp32, the output is bf16.  With N = 1 and a mask of one set bit it is ordinary
+ * On the way to the products only the softmax weights are rounded, to bf16 or finer (where a weight times the scale of its V
+ * is below 2^-28 of the largest such product: to 2^-39 of that), and elements of q that lie more than 2^38 below the largest
+ * of their row.  Sums and statistics are fp32, the output is bf16.  With N = 1 and a mask of one set bit it is ordinary
  * single-token decoding.  Everything else is as for gsd_verify_attn: literal mask bits, rows at positions >=
- * seq_lens[b] never reach the result whatever their codes and exponents are, a row with no visible key yields zeros.
- * Exponents below -117 or above 119 and e4m3's NaN codes are not expected in visible rows.
+ * seq_lens[b] never reach the result whatever their codes and exponents are, nor do draft rows that no node sees, and
+ * a row with no visible key yields zeros.  Exponents outside [-117, 119] are not expected in visible blocks.
  *
  *   q, draft_k, draft_v, ancestor_mask, seq_lens, out, workspace, status, stream   as for gsd_verify_attn
  *   k_cache, v_cache  [B, Lmax, Hkv, D] codes  device  in, 16-byte aligned

@@ -250,11 +250,38 @@ int attn_q8_params_ok(const gsd_attn_params* p, const gsd_kv8_params* c) {
     const int ok = attn_params_ok(p);
     if (ok != GSD_OK) return ok;
     if (!c) return GSD_ERR_NULL_POINTER;
+    if (p->kernel == GSD_ATTN_TCGEN05 && 128 % (p->Hq / p->Hkv) != 0) {
+        set_error_text("GSD_ATTN_TCGEN05 needs D == 128 and a group size that divides 128");
+        return GSD_ERR_UNSUPPORTED;
+    }
     return kv8_block_log2(c) < 0 ? GSD_ERR_BAD_SHAPE : GSD_OK;
 }
 
-// Few stacked rows: items of 16 or 32 of them, key ranges for as many CTAs as the device holds.
+int attn_q8_pick_kernel(const gsd_attn_params* p) {
+    if (p->kernel != GSD_ATTN_AUTO) return p->kernel;
+    const int G = p->Hq / p->Hkv;
+    return attn_tcgen05_supports(p->D, G) && p->N * G > 32 ? GSD_ATTN_TCGEN05 : GSD_ATTN_MMA;
+}
+
+// Scratch of a call over an 8-bit cache: that of the plan, and for the tcgen05 kernel K and V rows widened to bf16 and a
+// copy of draft_v.
+struct Q8Scratch {
+    size_t plan, rows, draft;
+    size_t total() const { return plan + 2 * rows + draft; }
+};
+Q8Scratch attn_q8_scratch(const gsd_attn_params* p, const AttnPlan& pl) {
+    const bool tc = pl.kernel == GSD_ATTN_TCGEN05;
+    return {align_up(pl.ws_bytes, 256), tc ? align_up((size_t)p->B * p->Lmax * p->Hkv * p->D * 2, 256) : 0,
+            tc ? align_up((size_t)p->B * p->N * p->Hkv * p->D * 2, 256) : 0};
+}
 AttnPlan attn_q8_make_plan(const gsd_attn_params* p, int sm_count) {
+    if (attn_q8_pick_kernel(p) == GSD_ATTN_TCGEN05) {
+        gsd_attn_params as = *p;
+        as.kernel = GSD_ATTN_TCGEN05;
+        as.num_splits = std::max(p->num_splits, 0);
+        return attn_make_plan(&as, sm_count);
+    }
+    // Few stacked rows: items of 16 or 32 of them, key ranges for as many CTAs as the device holds.
     AttnPlan pl = {};
     const int R = p->N * (p->Hq / p->Hkv);
     pl.kernel = GSD_ATTN_MMA;
@@ -283,7 +310,7 @@ extern "C" size_t gsd_verify_attn_q8_workspace_bytes(const gsd_attn_params* p, c
     if (attn_q8_params_ok(p, c) != GSD_OK) return 0;
     DeviceInfo di;
     if (device_info(&di) != 0) return 0;
-    return attn_q8_make_plan(p, di.sm_count).ws_bytes;
+    return attn_q8_scratch(p, attn_q8_make_plan(p, di.sm_count)).total();
 }
 
 extern "C" int gsd_verify_attn_q8(const void* q, const void* k_cache, const void* v_cache, const int8_t* k_exp,
@@ -301,8 +328,10 @@ extern "C" int gsd_verify_attn_q8(const void* q, const void* k_cache, const void
     DeviceInfo di;
     if (device_info(&di) != 0) return GSD_ERR_CUDA;
     const AttnPlan plan = attn_q8_make_plan(p, di.sm_count);
-    if (plan.ws_bytes > 0) {
-        if (!workspace || workspace_bytes < plan.ws_bytes) return GSD_ERR_WORKSPACE;
+    const Q8Scratch scratch = attn_q8_scratch(p, plan);
+    const size_t need = scratch.total();
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need) return GSD_ERR_WORKSPACE;
         if (((uintptr_t)workspace & 255u) != 0) return GSD_ERR_MISALIGNED;
     }
     AttnArgs a;
@@ -316,7 +345,17 @@ extern "C" int gsd_verify_attn_q8(const void* q, const void* k_cache, const void
     a.stream = (cudaStream_t)stream;
     a.kv8.k_exp = k_exp; a.kv8.v_exp = v_exp; a.kv8.block_log2 = kv8_block_log2(c);
     a.kv8.blocks = (p->Lmax + c->block - 1) / c->block; a.kv8.int8 = c->format == GSD_KV8_INT8;
-    int rc = launch_attn_q8_mma(a);
+    int rc;
+    if (plan.kernel == GSD_ATTN_TCGEN05) {
+        char* rows = (char*)workspace + scratch.plan;
+        if ((rc = launch_kv8_expand(a, rows, rows + scratch.rows, rows + 2 * scratch.rows)) != GSD_OK) return rc;
+        a.k_cache = rows;
+        a.v_cache = rows + scratch.rows;
+        a.draft_v = rows + 2 * scratch.rows;
+        rc = launch_attn_tcgen05(a);
+    } else {
+        rc = launch_attn_q8_mma(a);
+    }
     if (rc == GSD_OK && plan.slots > 0) rc = launch_attn_merge(a);
     return rc;
 }

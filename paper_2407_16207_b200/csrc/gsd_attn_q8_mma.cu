@@ -12,11 +12,11 @@
 // What bounds it: the one read of the codes.  Every warp has tiles of 16 keys of its own, a ring of them in shared
 // memory filled by asynchronous copies and nothing to wait for but its own; the warps meet once, at the end.
 // Widening costs one conversion for two e4m3 codes, and five integer or half instructions for four int8 codes.
-// (By way of bf16, with the scale multiplied in, an SM widened 39 codes a cycle, 77 this way; the copy rate is 23.)
 //
 // A lane takes its operands from whole 16-byte pieces of a row: the order of the head dimension inside a product
 // is free (queries are loaded in the same order), and so is the order of the output columns.
 #include "gsd_internal.cuh"
+#include "gsd_kv8.cuh"
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -26,7 +26,6 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kKeys = 16;                    // keys of a warp's tile
-constexpr int kLiftBits = 14;                // what weights and query rows are brought up by, see above
 
 struct Q8Params {
     const __nv_bfloat16 *q, *draft_k, *draft_v;
@@ -97,25 +96,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    uint32_t d;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-// Four codes -> two pairs of fp16, in order.
-template <bool INT8>
-__device__ __forceinline__ void widen(uint32_t w, uint32_t& p0, uint32_t& p1) {
-    if constexpr (INT8) {
-        // 0x6400 | u is 1024 + u for a byte u; u = code + 128
-        w ^= 0x80808080u;
-        const uint32_t x0 = __byte_perm(w, 0x64646464u, 0x4140), x1 = __byte_perm(w, 0x64646464u, 0x4342);
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(p0) : "r"(x0), "r"(0x64806480u));
-        asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(p1) : "r"(x1), "r"(0x64806480u));
-    } else {
-        asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(p0), "=r"(p1) : "r"(w));
-    }
-}
-
 template <int D, int MT, bool INT8>
 __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_kernel(Q8Params p) {
     using T = Q8Geo<D, MT>;
@@ -213,9 +193,9 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
             for (int x = 0; x < D / 8; ++x) top = max(top, max((w[x] & 0x7FFFu), (w[x] >> 16) & 0x7FFFu));
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const int ex = max((int)(top >> 7) - 127, -100);                             // 2^ex <= maximum < 2^(ex + 1)
-            const float lift = __int_as_float((127 + kLiftBits - min(ex, 126)) << 23);
-            row_mult[mt][h] = p.scale_log2 * __int_as_float((127 - kLiftBits + min(ex, 126)) << 23);
+            const int ex = lift_exp(top);
+            const float lift = two(kLiftBits - ex);
+            row_mult[mt][h] = p.scale_log2 * two(ex - kLiftBits);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -272,7 +252,6 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
                 }
         }
     };
-    auto two = [](int e) { return __int_as_float((e + 127) << 23); };                    // 2^e, -126 <= e <= 127
 
     for (int i = 0; i < n_prefix; ++i) {
         if (i + ST - 1 < n_prefix) issue(i + ST - 1);
@@ -396,12 +375,13 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
                     if (N - key0 < kKeys) w &= (1u << (N - key0)) - 1u;
                     any |= bits[mt][h] = w & 0xFFFFu;
                 }
-            if (!__any_sync(0xFFFFFFFFu, any != 0)) continue;
+            const uint32_t seen = __reduce_or_sync(0xFFFFFFFFu, any);     // keys that any row sees: others are not read
+            if (!seen) continue;
             float s[MT][2][4];
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) {
                 const int key = key0 + nt * 8 + i8;
-                const bool ok = key < N;
+                const bool ok = (seen >> (nt * 8 + i8)) & 1u;
                 const __nv_bfloat16* src = dk + (size_t)(ok ? key : 0) * row_bytes + j4 * 16;
                 uint32_t kw[D / 8];
 #pragma unroll
@@ -443,8 +423,8 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
                 uint32_t w[4][4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int key = key0 + 2 * j4 + (x & 1) + (x >> 1) * 8;
-                    const bool ok = key < N;
+                    const int at = 2 * j4 + (x & 1) + (x >> 1) * 8, key = key0 + at;
+                    const bool ok = (seen >> at) & 1u;
                     const uint4 v = ok ? *reinterpret_cast<const uint4*>(dv + (size_t)key * row_bytes + i8 * (D / 8) + y * 8) : make_uint4(0, 0, 0, 0);
                     w[x][0] = v.x; w[x][1] = v.y; w[x][2] = v.z; w[x][3] = v.w;
                 }

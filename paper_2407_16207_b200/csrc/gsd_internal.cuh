@@ -207,6 +207,9 @@ constexpr int kSeqPlanMaxSplit = 32;
 int launch_attn_plan(const AttnArgs& a);      // plans made on the device only: builds the table
 int launch_attn_mma(const AttnArgs& a);
 int launch_attn_q8_mma(const AttnArgs& a);
+// The visible rows of an 8-bit cache as bf16 rows [B, Lmax, Hkv, D] (rows past the end are left as they were), and draft_v with
+// zeros for rows that no node sees.
+int launch_kv8_expand(const AttnArgs& a, void* k_out, void* v_out, void* draft_v_out);
 int attn_q8_mma_rows(int R);                  // stacked rows of one of its items
 int attn_q8_mma_resident(int R);              // its CTAs an SM holds
 int launch_attn_tcgen05(const AttnArgs& a);

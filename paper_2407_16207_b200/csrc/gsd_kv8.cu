@@ -15,6 +15,7 @@
 // dependent trips to memory (length and path, then the rows) for accepted paths; those go to one cluster of CTAs per
 // sequence, which may advance seq_lens itself once every CTA of it has read the old length.
 #include "gsd_internal.cuh"
+#include "gsd_kv8.cuh"
 #include <initializer_list>
 
 namespace gsd {
@@ -40,7 +41,6 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
     asm("max.u16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
-__device__ __forceinline__ float two(int e) { return __int_as_float((e + 127) << 23); }     // 2^e, -126 <= e <= 127
 
 // Four values in units of the scale -> four codes.
 template <bool INT8>

@@ -3,8 +3,9 @@
 Tolerance of an element: the output's rounding, 2^-8 of it; the weights' rounding to bf16, 2^-8 of sum p |v|; and what the
 scores' errors do to the weights.  A score is an fp32 sum of D <= 128 products: off by at most 128 * 2^-23 of S = scale *
 sum |q k|, i.e. 2^-16 S, which moves a weight by that much of itself and the sum it is divided by likewise: 2^-15 S, and
-2^-20 for the exponential and the sums.  Weights are held in fp16 in units of 2^-14 and of the largest scale 2^e of the
-head's visible V: the smallest ones are off by half of 2^-24 of the unit, 2^-39 2^e, and there are L of them."""
+2^-20 for the exponential and the sums.  Over the codes weights are held in fp16 in units
+of 2^-14 and of the largest scale 2^e of the head's V: the smallest ones are off by half of 2^-24 of the unit, 2^-39 2^e, and
+there are L of them."""
 import numpy as np
 import pytest
 import torch
@@ -190,6 +191,32 @@ def test_agrees_with_the_bf16_call():
     got = call(x)
     # both are within 2^-8 (weights) and 2^-8 (output) of the same values, which are below 8 here
     assert (got.float() - ref.float()).abs().max() <= 4 * 2.0 ** -8 * float(want(x)[1].max())
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_draft_rows_that_nobody_sees_may_be_anything(kernel, bad):
+    x = make(12, 2, 40, 4, 2, 128, 100, [100, 0], "e4m3", 64)
+    x["see"][:, :, 5] = x["see"][:, :, 33] = x["see"][:, :, 39] = False
+    bits = np.zeros((2, 40, 64), bool)
+    bits[:, :, :40] = x["see"]
+    x["mask"] = np.packbits(bits, axis=2, bitorder="little").view(np.int32)
+    clean = {n: x[n].clone() for n in ("dk", "dv")}
+    for n in ("dk", "dv"):
+        x[n][:, [5, 33, 39]] = bad
+    got = call(x, kernel=kernel)
+    x.update(clean)
+    check(x, got)
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_draft_rows_of_any_size(kernel):
+    x = make(13, 1, 70, 4, 2, 128, 150, [150], "int8", 32)
+    for n in ("dk", "dv"):
+        x[n][:, ::3] = (x[n][:, ::3].float() * 2.0 ** -9).to(torch.bfloat16)
+    x["dv"][:, 1::7] = (x["dv"][:, 1::7].float() * 2.0 ** 12).to(torch.bfloat16)
+    x["dk"][:, 40:] = 0
+    check(x, call(x, kernel=kernel))
 
 
 def test_lengths_out_of_range_are_clamped_and_flagged():
