@@ -451,7 +451,7 @@ typedef struct gsd_kv8_params {
  *   K_j, V_j = draft_k, draft_v[b,j,c,:] for draft rows j with bit j of ancestor_mask[b][n] set
  *   out[b,n,h,:] = sum_j softmax_j(scale * <q[b,n,h,:], K_j>) * V_j
  * On the way to the products only the softmax weights are rounded, to bf16 or finer (where a weight times the scale of its V
- * is below 2^-28 of the largest such product: to 2^-39 of that), and elements of q that lie more than 2^38 below the largest
+ * is below 2^-22 of the largest such product: to 2^-33 of that), and elements of q that lie more than 2^38 below the largest
  * of their row.  Sums and statistics are fp32, the output is bf16.  With N = 1 and a mask of one set bit it is ordinary
  * single-token decoding.  Everything else is as for gsd_verify_attn: literal mask bits, rows at positions >=
  * seq_lens[b] never reach the result whatever their codes and exponents are, nor do draft rows that no node sees, and

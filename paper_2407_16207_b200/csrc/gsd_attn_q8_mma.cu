@@ -6,12 +6,14 @@
 // with K_j = c_j 2^(ek_j) and V_j = w_j 2^(ev_j).  The codes go to the tensor cores as they are, widened to fp16 (exact:
 // four and eight significant bits): ek is one factor of a tile's scores, ev one of its weights, so nothing is
 // multiplied per cache element.  fp16 holds a query row exactly once a power of two has brought its maximum to 2^14
-// (what falls below 2^-24 then is under 2^-38 of the maximum), and a weight p 2^(14 + ev - e_ref) to 11 bits, e_ref the
-// largest ev met so far; the accumulators are in units of 2^(e_ref - 14).
+// (what falls below 2^-24 then is under 2^-38 of the maximum), and a weight p 2^(8 + ev - e_ref) to 11 bits, e_ref the
+// largest ev met so far; the accumulators are in units of 2^(e_ref - 8).
 //
-// What bounds it: the one read of the codes.  Every warp has tiles of 16 keys of its own, a ring of them in shared
-// memory filled by asynchronous copies and nothing to wait for but its own; the warps meet once, at the end.
-// Widening costs one conversion for two e4m3 codes, and five integer or half instructions for four int8 codes.
+// Every warp has tiles of 16 keys of its own, a ring of them in shared memory filled by asynchronous copies and nothing to
+// wait for but its own; the warps meet once, at the end.  What bounds it is instructions: 16 keys (4 KB) of eight rows
+// took 522 with rows as the 16 rows of a product (half of them empty); here both products are transposed, S^T = K Q^T and
+// O^T = V^T P^T, with 16 keys or columns and 8 rows each, weights turned round by a movmatrix.  A tile's maximum is looked
+// at row by row only when a score exceeds the running one by more than 2^7.
 //
 // A lane takes its operands from whole 16-byte pieces of a row: the order of the head dimension inside a product
 // is free (queries are loaded in the same order), and so is the order of the output columns.
@@ -26,6 +28,8 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kKeys = 16;                    // keys of a warp's tile
+constexpr int kWeightBits = 8;               // what weights are brought up by in fp16
+constexpr float kLag = 7.f;                  // the running maximum of a row may lag behind by this much (log2 units): weights stay below 2^15
 
 struct Q8Params {
     const __nv_bfloat16 *q, *draft_k, *draft_v;
@@ -44,16 +48,18 @@ struct Q8Params {
     float scale_log2;
 };
 
-template <int D, int MT>
+template <int D, int NT>
 struct Q8Geo {
-    static constexpr int ROWS = 16 * MT;                        // stacked rows of an item
+    static constexpr int ROWS = 8 * NT;                         // stacked rows of an item
     static constexpr int TILE = kKeys * D;                      // bytes of a K or V tile
-    static constexpr int STAGES = MT == 1 ? 3 : D == 128 ? 5 : 6;
-    static constexpr int BLOCKS = MT == 1 ? 2 : 1;              // CTAs an SM
+    static constexpr int BLOCKS = NT <= 2 ? 2 : 1;              // CTAs an SM
+    static constexpr int STAGES = NT <= 2 ? 3 : 5;
     static constexpr int RING = kWarps * STAGES * 2 * TILE;
-    static constexpr int VALUES = MT * (D / 8 * 4 + 4);         // of a thread, when the warps' results are brought together
+    static constexpr int MTILES = D / 16;                       // output tiles of 16 columns
+    static constexpr int VALUES = NT * (MTILES * 4 + 4);        // of a thread, when the warps' results are brought together
     static constexpr int MEET = kWarps * VALUES * 32 * 4;
-    static constexpr int SMEM = RING > MEET ? RING : MEET;
+    static constexpr int Q_AT = RING > MEET ? RING : MEET;      // query fragments: [row group][k-step][lane] pairs of registers
+    static constexpr int SMEM = Q_AT + NT * (D / 16) * 32 * 8;
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -96,11 +102,18 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
-template <int D, int MT, bool INT8>
-__global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_kernel(Q8Params p) {
-    using T = Q8Geo<D, MT>;
-    constexpr int KS = D / 16;              // k-steps of the QK^T product
-    constexpr int DT = D / 8;               // output n-tiles
+// 8x8 fp16 or bf16 values, a row a quarter of lanes -> their transpose.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+
+template <int D, int NT, bool INT8>
+__global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_kernel(Q8Params p) {
+    using T = Q8Geo<D, NT>;
+    constexpr int KS = D / 16;              // k-steps of the product with K
+    constexpr int MTL = T::MTILES;          // output tiles
     constexpr int ST = T::STAGES;
     extern __shared__ __align__(128) unsigned char smem[];
 
@@ -130,9 +143,7 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
     // ---- the ring: K and V tiles of 16 rows, 16-byte pieces swizzled for the reads below
     const uint32_t ring = smem_u32(smem) + warp * (ST * 2 * T::TILE);
     const size_t row_bytes = (size_t)p.Hkv * D;
-    const uint8_t* kbase = p.k_cache + ((size_t)b * p.Lmax * p.Hkv + c) * D;
-    const uint8_t* vbase = p.v_cache + ((size_t)b * p.Lmax * p.Hkv + c) * D;
-    constexpr int PIECES = D / 16;                                                       // of a row
+    constexpr int PIECES = D / 16, LANE_ROWS = 32 / PIECES;                              // of a row; rows a copy of the warp takes
     auto k_off = [](int r, int ch) -> uint32_t {
         if (D == 128) return (uint32_t)(r * 128 + ((ch ^ ((r & 1) << 2)) << 4));
         return (uint32_t)((r >> 1) * 128 + ((((r & 1) << 2) + ch) << 4));
@@ -141,21 +152,26 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
         if (D == 128) return (uint32_t)(r * 128 + ((ch ^ (r & 6)) << 4));
         return (uint32_t)((r >> 1) * 128 + (((((r & 1) << 2) + ch) ^ (((r >> 1) & 3) << 1)) << 4));
     };
-    auto issue = [&](int i) {
-        const int key0 = (first + i * kWarps) * kKeys;
-        const uint32_t sk = ring + (i % ST) * (2 * T::TILE), sv = sk + T::TILE;
+    // where the lane's pieces of the next tile to be copied come from
+    const int my_row = lane / PIECES, my_piece = lane % PIECES;
+    int copy_key = first * kKeys + my_row;
+    const uint8_t* copy_k = p.k_cache + ((size_t)b * p.Lmax * p.Hkv + c) * D + (size_t)copy_key * row_bytes + my_piece * 16;
+    const ptrdiff_t k_to_v = p.v_cache - p.k_cache;
+    auto issue = [&](uint32_t stage) {
 #pragma unroll
-        for (int x = 0; x < kKeys * PIECES / 32; ++x) {
-            const int at = x * 32 + lane, r = at / PIECES, ch = at % PIECES;
-            const bool ok = key0 + r < L && GSD_IN_BOUNDS(key0 + r < p.Lmax && b < p.B && c < p.Hkv, p.status);
-            const size_t off = (size_t)(ok ? key0 + r : 0) * row_bytes + ch * 16;
-            cp_async16(sk + k_off(r, ch), kbase + off, ok ? 16 : 0);
-            cp_async16(sv + v_off(r, ch), vbase + off, ok ? 16 : 0);
+        for (int x = 0; x < kKeys / LANE_ROWS; ++x) {
+            const int r = x * LANE_ROWS + my_row;
+            const bool ok = copy_key + x * LANE_ROWS < L && GSD_IN_BOUNDS(copy_key + x * LANE_ROWS < p.Lmax && b < p.B && c < p.Hkv, p.status);
+            const uint8_t* src = ok ? copy_k + (size_t)(x * LANE_ROWS) * row_bytes : p.k_cache;
+            cp_async16(stage + k_off(r, my_piece), src, ok ? 16 : 0);
+            cp_async16(stage + T::TILE + v_off(r, my_piece), src + k_to_v, ok ? 16 : 0);
         }
+        copy_key += kWarps * kKeys;
+        copy_k += (size_t)(kWarps * kKeys) * row_bytes;
     };
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) {
-        if (s < n_prefix) issue(s);
+        if (s < n_prefix) issue(ring + s * (2 * T::TILE));
         cp_async_commit();
     }
     // The exponents of the warp's next 32 tiles, a tile a lane (a tile lies in one block: 16 divides a block).
@@ -169,93 +185,106 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
     };
     int exps = 0, exps_next = load_exps(0);
 
-    // ---- the query rows as fp16 fragments, each lifted by a power of two
-    uint32_t qf[MT][KS][4];
-    float row_mult[MT][2];
-    bool rvalid[MT][2];
-    const __nv_bfloat16* qrow[MT][2];
+    // ---- the query rows as fp16 fragments (rows are columns of the products), each lifted by a power of two: a warp for
+    // every eight rows puts them where all warps find them
+    __shared__ float s_mult[NT * 8];
+    const uint32_t q_at = smem_u32(smem) + T::Q_AT + lane * 8;
+    if (warp < NT) {
+        const int row = row0 + warp * 8 + i8;
+        const bool in = row < R;
+        const int rr = in ? row : 0;
+        const __nv_bfloat16* q = p.q + (((size_t)b * N + rr / G) * p.Hq + c * G + rr % G) * D + j4 * 16;
+        uint32_t w[D / 8];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+        for (int x = 0; x < D / 32; ++x) {
+            const uint4 v = in ? *reinterpret_cast<const uint4*>(q + (x >> 1) * 64 + (x & 1) * 8) : make_uint4(0, 0, 0, 0);
+            w[x * 4] = v.x; w[x * 4 + 1] = v.y; w[x * 4 + 2] = v.z; w[x * 4 + 3] = v.w;
+        }
+        uint32_t top = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int row = row0 + mt * 16 + h * 8 + i8;
-            rvalid[mt][h] = row < R;
-            const int rr = rvalid[mt][h] ? row : 0;
-            qrow[mt][h] = p.q + (((size_t)b * N + rr / G) * p.Hq + c * G + rr % G) * D + j4 * 16;
-            uint32_t w[D / 8];
+        for (int x = 0; x < D / 8; ++x) top = max(top, max((w[x] & 0x7FFFu), (w[x] >> 16) & 0x7FFFu));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const int ex = lift_exp(top);
+        const float lift = two(kLiftBits - ex);
+        if (j4 == 0) s_mult[warp * 8 + i8] = p.scale_log2 * two(ex - kLiftBits);
+        auto half2 = [&](uint32_t v) { return pack_f16(__uint_as_float(v << 16) * lift, __uint_as_float(v & 0xFFFF0000u) * lift); };
 #pragma unroll
-            for (int x = 0; x < D / 32; ++x) {
-                const uint4 v = rvalid[mt][h] ? *reinterpret_cast<const uint4*>(qrow[mt][h] + (x >> 1) * 64 + (x & 1) * 8) : make_uint4(0, 0, 0, 0);
-                w[x * 4] = v.x; w[x * 4 + 1] = v.y; w[x * 4 + 2] = v.z; w[x * 4 + 3] = v.w;
-            }
-            uint32_t top = 0;
+        for (int ks = 0; ks < KS; ++ks)
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(q_at + (warp * KS + ks) * 256), "r"(half2(w[ks * 2])), "r"(half2(w[ks * 2 + 1])) : "memory");
+    }
+    __syncthreads();
+    uint2 qf[NT == 1 ? KS : 1];
+    if (NT == 1) {
 #pragma unroll
-            for (int x = 0; x < D / 8; ++x) top = max(top, max((w[x] & 0x7FFFu), (w[x] >> 16) & 0x7FFFu));
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const int ex = lift_exp(top);
-            const float lift = two(kLiftBits - ex);
-            row_mult[mt][h] = p.scale_log2 * two(ex - kLiftBits);
+        for (int ks = 0; ks < KS; ++ks) qf[NT == 1 ? ks : 0] = lds64(q_at + ks * 256);
+    }
+    float row_mult[NT][2];                  // of the rows whose scores the thread holds: 8 nt + 2 j4 + {0, 1}
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+    for (int nt = 0; nt < NT; ++nt) {
+        row_mult[nt][0] = s_mult[nt * 8 + 2 * j4];
+        row_mult[nt][1] = s_mult[nt * 8 + 2 * j4 + 1];
+    }
+
+    float o[NT][MTL][4];                    // columns (D / 8) i8 + 2 mt and the one behind it, of the thread's two rows
+    float m_run[NT][2], l_run[NT][2];       // l: the lane's own keys
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int mt = 0; mt < MTL; ++mt) o[nt][mt][0] = o[nt][mt][1] = o[nt][mt][2] = o[nt][mt][3] = 0.f;
+        m_run[nt][0] = m_run[nt][1] = -CUDART_INF_F;
+        l_run[nt][0] = l_run[nt][1] = 0.f;
+    }
+    int e_ref = -126;                                                                    // accumulators: units of 2^(e_ref - kWeightBits)
+
+    // Products s (times mult[.][.]: log2 units; hidden ones -inf) -> weights 2^(s - m + shift) in place.  The running maximum is
+    // raised when a score exceeds it by more than kLag; the accumulators then follow, as they do a larger unit.
+    auto softmax = [&](float (&s)[NT][4], const float (&mult)[NT][2], float unit_back, float shift, float unshift) {
+        bool raise = unit_back != 1.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) raise |= fmaxf(s[nt][e], s[nt][e + 2]) * mult[nt][e] > m_run[nt][e] + kLag;
+        if (__any_sync(0xFFFFFFFFu, raise)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float a[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t v = w[ks * 2 + e];
-                    qf[mt][ks][h + 2 * e] = pack_f16(__uint_as_float(v << 16) * lift, __uint_as_float(v & 0xFFFF0000u) * lift);
+                    float mx = fmaxf(s[nt][e], s[nt][e + 2]) * mult[nt][e];
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+                    const float m_new = fmaxf(m_run[nt][e], mx), m_use = m_new == -CUDART_INF_F ? 0.f : m_new;   // (nothing visible yet)
+                    a[e] = fast_exp2(m_run[nt][e] - m_use);
+                    m_run[nt][e] = m_new;
+                    l_run[nt][e] *= a[e];
+                    a[e] *= unit_back;
                 }
-        }
-
-    float o[MT][DT][4];
-    float m_run[MT][2], l_run[MT][2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[mt][dt][0] = o[mt][dt][1] = o[mt][dt][2] = o[mt][dt][3] = 0.f;
-        m_run[mt][0] = m_run[mt][1] = -CUDART_INF_F;
-        l_run[mt][0] = l_run[mt][1] = 0.f;
-    }
-    int e_ref = -126;                                                                    // accumulators: units of 2^(e_ref - kLiftBits)
-
-    // Scores (log2 units, hidden ones -inf) -> weights in place; the accumulators follow a raised maximum or unit.
-    auto softmax = [&](float (&s)[MT][2][4], float unit_back) {
-        bool raised = unit_back != 1.f;
-        float alpha[MT][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float mx = fmaxf(fmaxf(s[mt][0][2 * h], s[mt][0][2 * h + 1]), fmaxf(s[mt][1][2 * h], s[mt][1][2 * h + 1]));
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
-                const float m_new = fmaxf(m_run[mt][h], mx);
-                const float m_use = m_new == -CUDART_INF_F ? 0.f : m_new;                // nothing visible yet
-                alpha[mt][h] = fast_exp2(m_run[mt][h] - m_use);
-                raised |= m_new != m_run[mt][h];
-                m_run[mt][h] = m_new;
-                float sum = 0.f;
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    s[mt][nt][2 * h] = fast_exp2(s[mt][nt][2 * h] - m_use);
-                    s[mt][nt][2 * h + 1] = fast_exp2(s[mt][nt][2 * h + 1] - m_use);
-                    sum += s[mt][nt][2 * h] + s[mt][nt][2 * h + 1];
+                for (int mt = 0; mt < MTL; ++mt) {
+                    o[nt][mt][0] *= a[0]; o[nt][mt][2] *= a[0];
+                    o[nt][mt][1] *= a[1]; o[nt][mt][3] *= a[1];
                 }
-                l_run[mt][h] = l_run[mt][h] * alpha[mt][h] + sum;
             }
-        if (__any_sync(0xFFFFFFFFu, raised)) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const float a0 = alpha[mt][0] * unit_back, a1 = alpha[mt][1] * unit_back;
-                    o[mt][dt][0] *= a0; o[mt][dt][1] *= a0;
-                    o[mt][dt][2] *= a1; o[mt][dt][3] *= a1;
-                }
         }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float off = shift - (m_run[nt][e] == -CUDART_INF_F ? 0.f : m_run[nt][e]);
+                s[nt][e] = fast_exp2(fmaf(s[nt][e], mult[nt][e], off));
+                s[nt][e + 2] = fast_exp2(fmaf(s[nt][e + 2], mult[nt][e], off));
+                l_run[nt][e] = fmaf(s[nt][e] + s[nt][e + 2], unshift, l_run[nt][e]);
+            }
     };
 
+    uint32_t stage = ring, fill = ring + (ST - 1) * (2 * T::TILE);
+    const uint32_t ring_end = ring + ST * (2 * T::TILE);
+#pragma unroll 1
     for (int i = 0; i < n_prefix; ++i) {
-        if (i + ST - 1 < n_prefix) issue(i + ST - 1);
+        if (i + ST - 1 < n_prefix) issue(fill);
         cp_async_commit();
+        fill = stage;
         if ((i & 31) == 0) {
             exps = exps_next;
             exps_next = load_exps(i + 32);
@@ -264,57 +293,70 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
         const int ek = max((int)(int8_t)(ex & 255), -126), ev = max(ex >> 8, -126);
         cp_async_wait<ST - 1>();
         __syncwarp();
-        const uint32_t sk = ring + (i % ST) * (2 * T::TILE), sv = sk + T::TILE;
+        const uint32_t sk = stage, sv = stage + T::TILE;
+        stage += 2 * T::TILE;
+        if (stage == ring_end) stage = ring;
 
-        float s[MT][2][4];
+        // S^T = K Q^T: 16 keys (i8, i8 + 8) x 8 rows; two chains at least
+        constexpr int CHAINS = NT == 1 ? 2 : 1;
+        float s[NT][4], s1[CHAINS][4];
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
+            for (int e = 0; e < 4; ++e) s[nt][e] = s1[0][e] = 0.f;
 #pragma unroll
-            for (int x = 0; x < D / 64; ++x) {
-                const uint4 kw = lds128(sk + k_off(nt * 8 + i8, x * 4 + j4));
-                const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w};
+        for (int x = 0; x < D / 64; ++x) {
+            const uint4 k0 = lds128(sk + k_off(i8, x * 4 + j4)), k1 = lds128(sk + k_off(8 + i8, x * 4 + j4));
+            const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    uint32_t b0, b1;
-                    widen<INT8>(w[y], b0, b1);
+            for (int y = 0; y < 4; ++y) {
+                uint32_t a[4];
+                widen<INT8>(w0[y], a[0], a[2]);
+                widen<INT8>(w1[y], a[1], a[3]);
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) mma_f16(s[mt][nt], qf[mt][x * 4 + y], b0, b1);
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint2 q = NT == 1 ? qf[NT == 1 ? x * 4 + y : 0] : lds64(q_at + (nt * KS + x * 4 + y) * 256);
+                    mma_f16(NT == 1 && (y & 1) ? s1[0] : s[nt], a, q.x, q.y);
                 }
             }
         }
-        const int key0 = (first + i * kWarps) * kKeys;
+        float mult[NT][2];
         const float sk2 = two(ek);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt) {
+            mult[nt][0] = row_mult[nt][0] * sk2;
+            mult[nt][1] = row_mult[nt][1] * sk2;
+            if (NT == 1) {
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+                for (int e = 0; e < 4; ++e) s[nt][e] += s1[0][e];
+            }
+        }
+        const int key = (first + i * kWarps) * kKeys + i8;
+        if (key - i8 + kKeys > L) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[mt][nt][e] *= row_mult[mt][e >> 1] * sk2;
-        if (key0 + kKeys > L) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (key0 + nt * 8 + j4 * 2 + (e & 1) >= L) s[mt][nt][e] = -CUDART_INF_F;
+                for (int e = 0; e < 2; ++e) {
+                    mult[nt][e] = fmaxf(mult[nt][e], 1.2e-38f);                          // (0 times -inf)
+                    if (key >= L) s[nt][e] = -CUDART_INF_F;
+                    if (key + 8 >= L) s[nt][e + 2] = -CUDART_INF_F;
+                }
         }
         float back = 1.f;
         if (ev > e_ref) {
             back = two(max(e_ref - ev, -126));                                           // (below 2^-126 of the unit: nothing is left)
             e_ref = ev;
         }
-        softmax(s, back);
-        const float lift = two(max(kLiftBits + ev - e_ref, -126));
-        uint32_t pf[MT][4];
+        // (a block far below the unit: its weights vanish in fp16 but still count in the sum)
+        const int shift = max(ev - e_ref + kWeightBits, -40);
+        softmax(s, mult, back, (float)shift, two(-shift));
+        uint32_t pf[NT][2];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-                pf[mt][x] = pack_f16(s[mt][x >> 1][(x & 1) * 2] * lift, s[mt][x >> 1][(x & 1) * 2 + 1] * lift);
-        // V: the lane's keys are 2 j4, 2 j4 + 1, and these + 8; its column in n-tile dt is i8 * (D / 8) + dt
+        for (int nt = 0; nt < NT; ++nt) {
+            pf[nt][0] = transpose8(pack_f16(s[nt][0], s[nt][1]));
+            pf[nt][1] = transpose8(pack_f16(s[nt][2], s[nt][3]));
+        }
+        // O^T += V^T P^T: the lane's keys are 2 j4, 2 j4 + 1, and these + 8; its columns (D / 8) i8 + 2 mt and the one behind
         uint32_t vw[4][D / 32];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -331,14 +373,11 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
         for (int y = 0; y < D / 32; ++y)
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
-                uint32_t a0, a1, c0, c1;
-                widen<INT8>(__byte_perm(vw[0][y], vw[1][y], z ? 0x7362 : 0x5140), a0, a1);
-                widen<INT8>(__byte_perm(vw[2][y], vw[3][y], z ? 0x7362 : 0x5140), c0, c1);
+                uint32_t a[4];
+                widen<INT8>(__byte_perm(vw[0][y], vw[1][y], z ? 0x7362 : 0x5140), a[0], a[1]);
+                widen<INT8>(__byte_perm(vw[2][y], vw[3][y], z ? 0x7362 : 0x5140), a[2], a[3]);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    mma_f16(o[mt][y * 4 + z * 2], pf[mt], a0, c0);
-                    mma_f16(o[mt][y * 4 + z * 2 + 1], pf[mt], a1, c1);
-                }
+                for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][y * 2 + z], a, pf[nt][0], pf[nt][1]);
             }
         __syncwarp();                       // the stage has been read: a copy may take its place
     }
@@ -346,184 +385,167 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, MT>::BLOCKS) attn_q8_mma_ke
 
     // ---- draft tiles: bf16 rows straight from global memory, by bf16 products
     if (n_prefix * kWarps + first < t_end) {
-        // (the unit of the accumulators: weights 2^(14 - e_ref) must fit bf16)
-        float back = 1.f;
+        // (the unit of the accumulators: weights 2^(kWeightBits - e_ref) must fit bf16)
         if (e_ref < -100) {
-            back = two(max(e_ref + 100, -126));
+            const float back = two(max(e_ref + 100, -126));
             e_ref = -100;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int mt = 0; mt < MTL; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[nt][mt][e] *= back;
         }
-        const float lift = two(kLiftBits - e_ref);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[mt][dt][e] *= back;
+        const float shift = (float)(kWeightBits - e_ref), unshift = two(max(e_ref - kWeightBits, -126));
         const __nv_bfloat16* dk = p.draft_k + ((size_t)b * N * p.Hkv + c) * D;
         const __nv_bfloat16* dv = p.draft_v + ((size_t)b * N * p.Hkv + c) * D;
 #pragma unroll 1
         for (int t = first + n_prefix * kWarps; t < t_end; t += kWarps) {
             const int key0 = (t - nPT) * kKeys;
-            uint32_t bits[MT][2], any = 0;
+            uint32_t bits[NT][2], any = 0;
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = row0 + mt * 16 + h * 8 + i8;
+                for (int e = 0; e < 2; ++e) {
+                    const int row = row0 + nt * 8 + 2 * j4 + e;
                     uint32_t w = 0;
-                    if (rvalid[mt][h]) w = p.mask[((size_t)b * N + row / G) * p.W + (key0 >> 5)] >> (key0 & 16);
+                    if (row < R) w = p.mask[((size_t)b * N + row / G) * p.W + (key0 >> 5)] >> (key0 & 16);
                     if (N - key0 < kKeys) w &= (1u << (N - key0)) - 1u;
-                    any |= bits[mt][h] = w & 0xFFFFu;
+                    any |= bits[nt][e] = w & 0xFFFFu;
                 }
             const uint32_t seen = __reduce_or_sync(0xFFFFFFFFu, any);     // keys that any row sees: others are not read
             if (!seen) continue;
-            float s[MT][2][4];
+            float s[NT][4], mult[NT][2];
+            uint32_t kw[2][D / 8];
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) {
-                const int key = key0 + nt * 8 + i8;
-                const bool ok = (seen >> (nt * 8 + i8)) & 1u;
-                const __nv_bfloat16* src = dk + (size_t)(ok ? key : 0) * row_bytes + j4 * 16;
-                uint32_t kw[D / 8];
+            for (int h = 0; h < 2; ++h) {
+                const int at = h * 8 + i8;
+                const bool ok = (seen >> at) & 1u;
+                const __nv_bfloat16* src = dk + (size_t)(ok ? key0 + at : 0) * row_bytes + j4 * 16;
 #pragma unroll
                 for (int x = 0; x < D / 32; ++x) {
                     const uint4 v = ok ? *reinterpret_cast<const uint4*>(src + (x >> 1) * 64 + (x & 1) * 8) : make_uint4(0, 0, 0, 0);
-                    kw[x * 4] = v.x; kw[x * 4 + 1] = v.y; kw[x * 4 + 2] = v.z; kw[x * 4 + 3] = v.w;
-                }
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    s[mt][nt][0] = s[mt][nt][1] = s[mt][nt][2] = s[mt][nt][3] = 0.f;
-#pragma unroll
-                    for (int x = 0; x < D / 32; ++x) {           // two k-steps: eight elements of either row
-                        uint4 v[2];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            v[h] = rvalid[mt][h] ? *reinterpret_cast<const uint4*>(qrow[mt][h] + (x >> 1) * 64 + (x & 1) * 8) : make_uint4(0, 0, 0, 0);
-                        const uint32_t a0[4] = {v[0].x, v[1].x, v[0].y, v[1].y}, a1[4] = {v[0].z, v[1].z, v[0].w, v[1].w};
-                        mma_bf16(s[mt][nt], a0, kw[x * 4], kw[x * 4 + 1]);
-                        mma_bf16(s[mt][nt], a1, kw[x * 4 + 2], kw[x * 4 + 3]);
-                    }
+                    kw[h][x * 4] = v.x; kw[h][x * 4 + 1] = v.y; kw[h][x * 4 + 2] = v.z; kw[h][x * 4 + 3] = v.w;
                 }
             }
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nt = 0; nt < NT; ++nt) {
+                const int row = row0 + nt * 8 + i8;
+                const bool in = row < R;
+                const __nv_bfloat16* q = p.q + (((size_t)b * N + (in ? row / G : 0)) * p.Hq + c * G + (in ? row % G : 0)) * D + j4 * 16;
+                s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+                mult[nt][0] = mult[nt][1] = p.scale_log2;
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
+                for (int x = 0; x < D / 32; ++x) {               // two k-steps: eight elements of a row
+                    const uint4 v = in ? *reinterpret_cast<const uint4*>(q + (x >> 1) * 64 + (x & 1) * 8) : make_uint4(0, 0, 0, 0);
+                    const uint32_t a0[4] = {kw[0][x * 4], kw[1][x * 4], kw[0][x * 4 + 1], kw[1][x * 4 + 1]};
+                    const uint32_t a1[4] = {kw[0][x * 4 + 2], kw[1][x * 4 + 2], kw[0][x * 4 + 3], kw[1][x * 4 + 3]};
+                    mma_bf16(s[nt], a0, v.x, v.y);
+                    mma_bf16(s[nt], a1, v.z, v.w);
+                }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[mt][nt][e] = (bits[mt][e >> 1] >> (nt * 8 + j4 * 2 + (e & 1))) & 1u ? s[mt][nt][e] * p.scale_log2 : -CUDART_INF_F;
-            softmax(s, 1.f);
-            uint32_t pf[MT][4];
+                for (int e = 0; e < 4; ++e)
+                    if (!((bits[nt][e & 1] >> (i8 + (e >> 1) * 8)) & 1u)) s[nt][e] = -CUDART_INF_F;
+            }
+            softmax(s, mult, 1.f, shift, unshift);
+            uint32_t pf[NT][2];
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int nt = 0; nt < NT; ++nt) {
+                pf[nt][0] = transpose8(pack_bf16(s[nt][0], s[nt][1]));
+                pf[nt][1] = transpose8(pack_bf16(s[nt][2], s[nt][3]));
+            }
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    pf[mt][x] = pack_bf16(s[mt][x >> 1][(x & 1) * 2] * lift, s[mt][x >> 1][(x & 1) * 2 + 1] * lift);
-#pragma unroll
-            for (int y = 0; y < D / 64; ++y) {                   // eight output n-tiles at a time
+            for (int y = 0; y < D / 64; ++y) {                   // eight columns of a lane at a time
                 uint32_t w[4][4];
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const int at = 2 * j4 + (x & 1) + (x >> 1) * 8, key = key0 + at;
+                    const int at = 2 * j4 + (x & 1) + (x >> 1) * 8;
                     const bool ok = (seen >> at) & 1u;
-                    const uint4 v = ok ? *reinterpret_cast<const uint4*>(dv + (size_t)key * row_bytes + i8 * (D / 8) + y * 8) : make_uint4(0, 0, 0, 0);
+                    const uint4 v = ok ? *reinterpret_cast<const uint4*>(dv + (size_t)(key0 + at) * row_bytes + i8 * (D / 8) + y * 8) : make_uint4(0, 0, 0, 0);
                     w[x][0] = v.x; w[x][1] = v.y; w[x][2] = v.z; w[x][3] = v.w;
                 }
 #pragma unroll
-                for (int z = 0; z < 4; ++z)
+                for (int z = 0; z < 4; ++z) {
+                    const uint32_t a[4] = {__byte_perm(w[0][z], w[1][z], 0x5410), __byte_perm(w[0][z], w[1][z], 0x7632),
+                                           __byte_perm(w[2][z], w[3][z], 0x5410), __byte_perm(w[2][z], w[3][z], 0x7632)};
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t b0 = __byte_perm(w[0][z], w[1][z], e ? 0x7632 : 0x5410), b1 = __byte_perm(w[2][z], w[3][z], e ? 0x7632 : 0x5410);
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) mma_bf16(o[mt][y * 8 + z * 2 + e], pf[mt], b0, b1);
-                    }
+                    for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][y * 4 + z], a, pf[nt][0], pf[nt][1]);
+                }
             }
         }
     }
 
     // ---- the warps' results meet in the memory of the rings, each warp brings a share of the columns together
-    const float in_units = two(e_ref) * two(-kLiftBits);           // (below 2^-126: one product, exact)
+    const float in_units = two(e_ref) * two(-kWeightBits);       // (below 2^-126: one product, exact)
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            l_run[mt][h] += __shfl_xor_sync(0xFFFFFFFFu, l_run[mt][h], 1);
-            l_run[mt][h] += __shfl_xor_sync(0xFFFFFFFFu, l_run[mt][h], 2);
-        }
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) l_run[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l_run[nt][e], x);
     float* const part = reinterpret_cast<float*>(smem) + lane;
-    auto part_of = [&](int w, int mt) { return part + (w * MT + mt) * (T::VALUES / MT * 32); };
+    auto part_of = [&](int w, int nt) { return part + (w * NT + nt) * (T::VALUES / NT * 32); };
     __syncthreads();
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        float* at = part_of(warp, mt);
+    for (int nt = 0; nt < NT; ++nt) {
+        float* at = part_of(warp, nt);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+        for (int mt = 0; mt < MTL; ++mt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) at[(dt * 4 + e) * 32] = o[mt][dt][e] * in_units;
+            for (int e = 0; e < 4; ++e) at[(mt * 4 + e) * 32] = o[nt][mt][e] * in_units;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            at[(DT * 4 + h) * 32] = m_run[mt][h];
-            at[(DT * 4 + 2 + h) * 32] = l_run[mt][h];
+        for (int e = 0; e < 2; ++e) {
+            at[(MTL * 4 + e) * 32] = m_run[nt][e];
+            at[(MTL * 4 + 2 + e) * 32] = l_run[nt][e];
         }
     }
     __syncthreads();
-    constexpr int SHARE = DT / kWarps;                           // n-tiles of a warp: columns i * DT + warp * SHARE + 0..SHARE - 1
+    // (D = 64: half as many output tiles as warps; the row groups are shared out too)
+    constexpr int SHARERS = kWarps / MTL;
+    const int mt = warp % MTL;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        float w[kWarps][2], m[2], l[2], r[SHARE][4];
+    for (int nt = 0; nt < NT; ++nt) {
+        if (SHARERS > 1 && nt % SHARERS != warp / MTL) continue;
+        float w[kWarps][2], m[2], l[2], r[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            m[h] = -CUDART_INF_F;
-            l[h] = 0.f;
+        for (int e = 0; e < 2; ++e) {
+            m[e] = -CUDART_INF_F;
+            l[e] = 0.f;
 #pragma unroll
             for (int k = 0; k < kWarps; ++k) {
-                w[k][h] = part_of(k, mt)[(DT * 4 + h) * 32];
-                m[h] = fmaxf(m[h], w[k][h]);
+                w[k][e] = part_of(k, nt)[(MTL * 4 + e) * 32];
+                m[e] = fmaxf(m[e], w[k][e]);
             }
-            const float m_use = m[h] == -CUDART_INF_F ? 0.f : m[h];
+            const float m_use = m[e] == -CUDART_INF_F ? 0.f : m[e];
 #pragma unroll
             for (int k = 0; k < kWarps; ++k) {
-                w[k][h] = fast_exp2(w[k][h] - m_use);
-                l[h] += w[k][h] * part_of(k, mt)[(DT * 4 + 2 + h) * 32];
+                w[k][e] = fast_exp2(w[k][e] - m_use);
+                l[e] += w[k][e] * part_of(k, nt)[(MTL * 4 + 2 + e) * 32];
             }
         }
 #pragma unroll
-        for (int dt = 0; dt < SHARE; ++dt)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                r[dt][e] = 0.f;
+            for (int k = 0; k < kWarps; ++k) r[e] += w[k][e & 1] * part_of(k, nt)[(mt * 4 + e) * 32];
+        const int col = i8 * (D / 8) + 2 * mt;
 #pragma unroll
-                for (int k = 0; k < kWarps; ++k) r[dt][e] += w[k][e >> 1] * part_of(k, mt)[((warp * SHARE + dt) * 4 + e) * 32];
-            }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (!rvalid[mt][h]) continue;
-            const int rloc = mt * 16 + h * 8 + i8, row = row0 + rloc;
+        for (int e = 0; e < 2; ++e) {
+            const int rloc = nt * 8 + 2 * j4 + e, row = row0 + rloc;
+            if (row >= R) continue;
             if (nsplit == 1) {
                 if (!GSD_IN_BOUNDS(b < p.B && c < p.Hkv && row < p.R, p.status)) continue;
-                const float inv = l[h] > 0.f ? 1.f / l[h] : 0.f;
-                __nv_bfloat16* dst = p.out + (((size_t)b * N + row / G) * p.Hq + c * G + row % G) * D;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int col = (j4 * 2 + e) * DT + warp * SHARE;
-                    if constexpr (SHARE == 2) *reinterpret_cast<uint32_t*>(dst + col) = pack_bf16(r[0][h * 2 + e] * inv, r[1][h * 2 + e] * inv);
-                    else dst[col] = __float2bfloat16_rn(r[0][h * 2 + e] * inv);
-                }
+                const float inv = l[e] > 0.f ? 1.f / l[e] : 0.f;
+                *reinterpret_cast<uint32_t*>(p.out + (((size_t)b * N + row / G) * p.Hq + c * G + row % G) * D + col) = pack_bf16(r[e] * inv, r[e + 2] * inv);
             } else {
                 if (!GSD_IN_BOUNDS(slot >= 0 && slot < p.slots, p.status)) continue;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int col = (j4 * 2 + e) * DT + warp * SHARE;
-                    float* dst = p.part_o + (((size_t)slot * (D / 4) + col / 4) * 64 + rloc) * 4 + col % 4;
-                    if constexpr (SHARE == 2) *reinterpret_cast<float2*>(dst) = make_float2(r[0][h * 2 + e], r[1][h * 2 + e]);
-                    else *dst = r[0][h * 2 + e];
-                }
-                if (warp == 0 && j4 == 0) *reinterpret_cast<float2*>(p.part_ml + ((size_t)slot * 64 + rloc) * 2) = make_float2(m[h], l[h]);
+                *reinterpret_cast<float2*>(p.part_o + (((size_t)slot * (D / 4) + col / 4) * 64 + rloc) * 4 + col % 4) = make_float2(r[e], r[e + 2]);
+                if (mt == 0 && i8 == 0) *reinterpret_cast<float2*>(p.part_ml + ((size_t)slot * 64 + rloc) * 2) = make_float2(m[e], l[e]);
             }
         }
     }
 }
 
-template <int D, int MT, bool INT8>
+template <int D, int NT, bool INT8>
 int launch_t(const AttnArgs& a) {
     Q8Params p;
     p.q = (const __nv_bfloat16*)a.q; p.draft_k = (const __nv_bfloat16*)a.draft_k; p.draft_v = (const __nv_bfloat16*)a.draft_v;
@@ -534,31 +556,40 @@ int launch_t(const AttnArgs& a) {
     p.scale_log2 = a.scale_log2; p.plan = a.plan.dev; p.slots = a.plan.slots;
     p.part_o = (float*)a.workspace;
     p.part_ml = (float*)((char*)a.workspace + plan_part_o_bytes(a.plan, a.D));
-    constexpr int smem = Q8Geo<D, MT>::SMEM;
+    constexpr int smem = Q8Geo<D, NT>::SMEM;
     {
         static bool done[64] = {};   // per template instance: the opt-in sticks per device
         int dev = 0;
         GSD_CUDA_TRY(cudaGetDevice(&dev));
         if (dev < 0 || dev >= 64 || !done[dev]) {
-            GSD_CUDA_TRY(cudaFuncSetAttribute(attn_q8_mma_kernel<D, MT, INT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+            GSD_CUDA_TRY(cudaFuncSetAttribute(attn_q8_mma_kernel<D, NT, INT8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
             if (dev >= 0 && dev < 64) done[dev] = true;
         }
     }
-    GSD_CUDA_TRY(launch_dependent(attn_q8_mma_kernel<D, MT, INT8>, dim3(a.plan.ctas), dim3(kThreads), smem, a.stream, p));
+    GSD_CUDA_TRY(launch_dependent(attn_q8_mma_kernel<D, NT, INT8>, dim3(a.plan.ctas), dim3(kThreads), smem, a.stream, p));
     return GSD_OK;
 }
-template <int D, int MT>
-int launch_fmt(const AttnArgs& a) { return a.kv8.int8 ? launch_t<D, MT, true>(a) : launch_t<D, MT, false>(a); }
+template <int D, int NT>
+int launch_fmt(const AttnArgs& a) { return a.kv8.int8 ? launch_t<D, NT, true>(a) : launch_t<D, NT, false>(a); }
 
 }  // namespace
 
-int attn_q8_mma_rows(int R) { return R <= 16 ? 16 : 32; }
+int attn_q8_mma_rows(int R) { return R <= 8 ? 8 : R <= 16 ? 16 : R <= 24 ? 24 : 32; }
 int attn_q8_mma_resident(int R) { return R <= 16 ? 2 : 1; }
 
+template <int D>
+static int launch_d(const AttnArgs& a) {
+    switch (a.plan.rows_per_item) {
+        case 8: return launch_fmt<D, 1>(a);
+        case 16: return launch_fmt<D, 2>(a);
+        case 24: return launch_fmt<D, 3>(a);
+        default: return launch_fmt<D, 4>(a);
+    }
+}
+
 int launch_attn_q8_mma(const AttnArgs& a) {
-    const bool one = a.plan.rows_per_item == 16;
-    if (a.D == 128) return one ? launch_fmt<128, 1>(a) : launch_fmt<128, 2>(a);
-    if (a.D == 64) return one ? launch_fmt<64, 1>(a) : launch_fmt<64, 2>(a);
+    if (a.D == 128) return launch_d<128>(a);
+    if (a.D == 64) return launch_d<64>(a);
     return GSD_ERR_BAD_SHAPE;
 }
 

@@ -4,7 +4,7 @@ Tolerance of an element: the output's rounding, 2^-8 of it; the weights' roundin
 scores' errors do to the weights.  A score is an fp32 sum of D <= 128 products: off by at most 128 * 2^-23 of S = scale *
 sum |q k|, i.e. 2^-16 S, which moves a weight by that much of itself and the sum it is divided by likewise: 2^-15 S, and
 2^-20 for the exponential and the sums.  Over the codes weights are held in fp16 in units
-of 2^-14 and of the largest scale 2^e of the head's V: the smallest ones are off by half of 2^-24 of the unit, 2^-39 2^e, and
+of 2^-8 and of the largest scale 2^e of the head's V: the smallest ones are off by half of 2^-24 of the unit, 2^-33 2^e, and
 there are L of them."""
 import numpy as np
 import pytest
@@ -74,7 +74,7 @@ def want(x, scale=None):
         spread.append(a)
         size.append(s)
         top = np.exp2(x["ve"][b][:-(-L // x["block"])].max(0, initial=-126).astype(float))              # [H]
-        floor.append(np.repeat(L * 2.0 ** -39 * top * kv8_ref.QMAX[x["fmt"]], x["Hq"] // x["Hkv"])[None, :, None])
+        floor.append(np.repeat(L * 2.0 ** -33 * top * kv8_ref.QMAX[x["fmt"]], x["Hq"] // x["Hkv"])[None, :, None])
     return np.stack(out), np.stack(spread), np.stack(size), np.stack(floor)
 
 
