@@ -534,7 +534,8 @@ int gsd_append_kv_q8(void* k_cache, void* v_cache, int8_t* k_exp, int8_t* v_exp,
  *   p             host; 0 <= k <= min(GSD_LOGPROBS_MAX_K, V)
  *   workspace     device scratch of gsd_token_logprobs_workspace_bytes(p) bytes, 8-byte aligned, arbitrary contents
  *   status        device int32 word or NULL (GSD_DEV_BAD_TOKEN, GSD_DEV_BAD_CSR for a node out of range, GSD_DEV_BAD_LOGITS)
- * The sums are fp32 (ex2.approx).  Asynchronous on `stream`, allocates nothing.
+ * The sums are fp32 (ex2.approx).  The same call gives the same bits; where a row is cut, and with it the order of its
+ * sums, depends on all of `lens`.  Asynchronous on `stream`, allocates nothing.
  */
 #define GSD_LOGPROBS_MAX_K 32
 typedef struct gsd_logprobs_params {

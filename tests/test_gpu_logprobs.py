@@ -117,6 +117,38 @@ def test_batches(B, N, T, V):
     check(x, nodes, tokens, lens, 5, got)
 
 
+@pytest.mark.parametrize("k", [0, 3, 32])
+def test_rows_shared_out_between_warps_that_take_more_than_one(k):
+    rng = np.random.default_rng(k)
+    B, N, T, V = 4, 60, 300, 20483                             # 1.3 to 7 loads of a warp, from the middle of a row to another's
+    x = (rng.standard_normal((B, N, V)) * 2).astype(np.float32)
+    x[1, 7] = 1.5
+    x[3, 5] = np.arange(V, dtype=np.float32) * np.float32(1e-3)
+    nodes, tokens = rng.integers(0, N, (B, T)), rng.integers(0, V, (B, T))
+    nodes[1, 20:25], nodes[3, 9] = 7, 5
+    for lens in ([300, 0, 211, 300], [0, 0, 0, 77], [0, 260, 0, 0]):
+        got, status = run(x, nodes, tokens, lens, k)
+        assert status == 0
+        seen = [min(n, 40) for n in lens]                      # (the oracle takes its time)
+        check(x, nodes[:, :40], tokens[:, :40], seen, k, [g[:, :40] for g in got])
+        for b in range(B):
+            if lens[b] > 40:
+                check(x[b:b + 1], nodes[b:b + 1, lens[b] - 9:lens[b]], tokens[b:b + 1, lens[b] - 9:lens[b]], [9], k, [g[b:b + 1, lens[b] - 9:lens[b]] for g in got])
+            assert (got[0][b, lens[b]:] == 0).all()
+
+
+@pytest.mark.parametrize("B", [1023, 1024, 1025, 2500])
+def test_more_sequences_than_a_group(B):
+    rng = np.random.default_rng(B)
+    T, V = 3, 41
+    x = rng.standard_normal((B, 2, V)).astype(np.float32)
+    nodes, tokens, lens = rng.integers(0, 2, (B, T)), rng.integers(0, V, (B, T)), rng.integers(0, T + 1, B)
+    lens[B // 2:B // 2 + 100] = 0
+    got, status = run(x, nodes, tokens, lens, 4)
+    assert status == 0
+    check(x, nodes, tokens, lens, 4, got)
+
+
 def test_lengths_are_clamped_and_outputs_may_be_given():
     x = np.random.default_rng(2).standard_normal((2, 3, 400)).astype(np.float32)
     out = (torch.full((2, 3), 7.0, device="cuda"), torch.full((2, 3), 7.0, device="cuda"),
