@@ -42,18 +42,33 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
     return d;
 }
 
-// Four values in units of the scale -> four codes.
+// Two values times f, as fp32 pairs (one instruction).
+__device__ __forceinline__ float2 scaled(float a, float b, float f) {
+    const float2 v = make_float2(a, b), s = make_float2(f, f);
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<const unsigned long long*>(&v)), "l"(*reinterpret_cast<const unsigned long long*>(&s)));
+    return *reinterpret_cast<float2*>(&d);
+}
+// Four values in units of the scale, of at most 11 significant bits -> four codes.
+// int8: the values are exact in fp16 (what is below its normal numbers becomes 0), and 1536 + x has x's nearest integer in its
+// lowest bits, ties to even.  A conversion to an integer per value, at a quarter of the rate, took 51.2 instead of
+// 44.4 us where 8 x 4096 tokens of 8 heads are appended.
 template <bool INT8>
-__device__ __forceinline__ uint32_t round4(float a, float b, float c, float d) {
+__device__ __forceinline__ uint32_t round4(float2 a, float2 b) {
+    uint32_t w;
     if constexpr (INT8) {
-        auto r = [](float x) { return (uint32_t)__float2int_rn(fminf(fmaxf(x, -127.f), 127.f)) & 255u; };
-        return r(a) | r(b) << 8 | r(c) << 16 | r(d) << 24;
+        uint32_t p[2];
+        const float2 v[2] = {a, b};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm("{\n .reg .b32 h;\n cvt.rn.satfinite.f16x2.f32 h, %2, %1;\n min.xorsign.abs.f16x2 h, h, %3;\n add.rn.f16x2 %0, h, %4;\n}"
+                : "=r"(p[i]) : "f"(v[i].x), "f"(v[i].y), "r"(0x57F057F0u), "r"(0x66006600u));      // 127, 1536
+        w = __byte_perm(p[0], p[1], 0x6420);
     } else {
-        uint32_t w;
         asm("{\n .reg .b16 l, h;\n cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n mov.b32 %0, {l, h};\n}"
-            : "=r"(w) : "f"(a), "f"(b), "f"(c), "f"(d));
-        return w;
+            : "=r"(w) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     }
+    return w;
 }
 // Four codes in units of another scale.
 template <bool INT8>
@@ -69,7 +84,7 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float f) {
         for (int i = 0; i < 2; ++i)
             asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(x[2 * i]), "=f"(x[2 * i + 1]) : "r"(p[i]));
     }
-    return round4<INT8>(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+    return round4<INT8>(scaled(x[0], x[1], f), scaled(x[2], x[3], f));
 }
 // The exponent that a largest magnitude (bf16 bits) asks for.
 template <bool INT8>
@@ -197,11 +212,8 @@ __global__ void __launch_bounds__(kThreads) kv8_write_kernel(WriteArgs a) {
             for (int k = 0; k < kPieces; ++k) {
                 const int at = k * group + t, pos = r0 + at / ROW_PIECES;
                 if (pos >= r1 || !GSD_IN_BOUNDS(pos >= 0 && pos < a.Lmax, a.status)) continue;
-                auto lo16 = [&](uint32_t w) { return __uint_as_float(w << 16) * f; };
-                auto hi16 = [&](uint32_t w) { return __uint_as_float(w & 0xFFFF0000u) * f; };
-                uint2 c;
-                c.x = round4<INT8>(lo16(x[k].x), hi16(x[k].x), lo16(x[k].y), hi16(x[k].y));
-                c.y = round4<INT8>(lo16(x[k].z), hi16(x[k].z), lo16(x[k].w), hi16(x[k].w));
+                auto both = [&](uint32_t w) { return scaled(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u), f); };
+                const uint2 c = make_uint2(round4<INT8>(both(x[k].x), both(x[k].y)), round4<INT8>(both(x[k].z), both(x[k].w)));
                 *reinterpret_cast<uint2*>(dst + (size_t)pos * a.Hkv * D + at % ROW_PIECES * 8) = c;
             }
             if (held && e > e_old) {
