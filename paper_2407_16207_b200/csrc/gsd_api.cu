@@ -297,7 +297,7 @@ AttnPlan attn_q8_make_plan(const gsd_attn_params* p, int sm_count) {
     pl.items = pl.dev.tiles_per_unit * p->B * p->Hkv;
     pl.dev.items_a = pl.items;
     pl.dev.splits_a = pl.dev.splits_b = 1;
-    const int resident = sm_count * attn_q8_mma_resident(R);
+    const int resident = sm_count * attn_q8_mma_resident(R, p->D);
     if (p->num_splits > 0) {
         pl.dev.splits_a = p->num_splits;
     } else if (pl.items < resident) {

@@ -52,8 +52,8 @@ template <int D, int NT>
 struct Q8Geo {
     static constexpr int ROWS = 8 * NT;                         // stacked rows of an item
     static constexpr int TILE = kKeys * D;                      // bytes of a K or V tile
-    static constexpr int BLOCKS = NT <= 2 ? 2 : 1;              // CTAs an SM
-    static constexpr int STAGES = NT <= 2 ? 3 : 5;
+    static constexpr int BLOCKS = NT <= 2 || (NT == 3 && D == 64) ? 2 : 1;   // CTAs an SM, as their registers allow
+    static constexpr int STAGES = BLOCKS == 2 && D == 128 ? 3 : 5;
     static constexpr int RING = kWarps * STAGES * 2 * TILE;
     static constexpr int MTILES = D / 16;                       // output tiles of 16 columns
     static constexpr int VALUES = NT * (MTILES * 4 + 4);        // of a thread, when the warps' results are brought together
@@ -173,6 +173,18 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
     for (int s = 0; s < ST - 1; ++s) {
         if (s < n_prefix) issue(ring + s * (2 * T::TILE));
         cp_async_commit();
+    }
+    // The draft tiles come last, as a chain of mask, keys and values: asked for from DRAM now.
+    for (int t = first + n_prefix * kWarps; t < t_end; t += kWarps) {
+        const int row = (t - nPT) * kKeys + (lane & 15);
+        if (row < N) {
+            const size_t at = (((size_t)b * N + row) * p.Hkv + c) * D;
+            const __nv_bfloat16* src = lane < 16 ? p.draft_k + at : p.draft_v + at;
+#pragma unroll
+            for (int x = 0; x < D; x += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + x) : "memory");
+        }
+        for (int node = row0 / G + lane; node <= min(row0 + T::ROWS - 1, R - 1) / G; node += 32)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.mask + ((size_t)b * N + node) * p.W + ((t - nPT) * kKeys >> 5)) : "memory");
     }
     // The exponents of the warp's next 32 tiles, a tile a lane (a tile lies in one block: 16 divides a block).
     auto load_exps = [&](int i0) -> int {
@@ -574,8 +586,15 @@ int launch_fmt(const AttnArgs& a) { return a.kv8.int8 ? launch_t<D, NT, true>(a)
 
 }  // namespace
 
-int attn_q8_mma_rows(int R) { return R <= 8 ? 8 : R <= 16 ? 16 : R <= 24 ? 24 : 32; }
-int attn_q8_mma_resident(int R) { return R <= 16 ? 2 : 1; }
+// As few items as 32 rows each allow, with the row groups shared out evenly.
+int attn_q8_mma_rows(int R) {
+    const int items = (R + 31) / 32, groups = (R + 7) / 8;
+    return 8 * ((groups + items - 1) / items);
+}
+int attn_q8_mma_resident(int R, int D) {
+    const int rows = attn_q8_mma_rows(R);
+    return rows <= 16 || (rows == 24 && D == 64) ? 2 : 1;
+}
 
 template <int D>
 static int launch_d(const AttnArgs& a) {

@@ -211,7 +211,7 @@ int launch_attn_q8_mma(const AttnArgs& a);
 // zeros for rows that no node sees.
 int launch_kv8_expand(const AttnArgs& a, void* k_out, void* v_out, void* draft_v_out);
 int attn_q8_mma_rows(int R);                  // stacked rows of one of its items
-int attn_q8_mma_resident(int R);              // its CTAs an SM holds
+int attn_q8_mma_resident(int R, int D);              // its CTAs an SM holds
 int launch_attn_tcgen05(const AttnArgs& a);
 bool attn_tcgen05_supports(int D, int G);
 int attn_tcgen05_rows(int G);                 // stacked rows of one row tile
