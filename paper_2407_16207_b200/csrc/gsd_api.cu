@@ -260,7 +260,7 @@ int attn_q8_params_ok(const gsd_attn_params* p, const gsd_kv8_params* c) {
 // The few-row kernel reads the cache once for 32 rows, one CTA an SM beyond 16; the tcgen05 kernel pays for the widening of
 // every row first.  us, few-row and tcgen05, D 128: 8 x 64/8 heads, L 2048, R = 32 22.8 and 42.3, R = 64 (128 items) 30.1 and
 // 42.3, R = 96 56.7 and 43.4; 4 x 32 heads, L 1000, R = 32 23.2 and 38.7, R = 40 (256 items) 41.0 and 39.1; 1 x 32, L 2048, R = 64
-// 22.9 and 26.2, R = 96 30.4 and 27.7; 1 x 64/8, L 16384, R = 64 29.1 and 39.7, R = 128 45.2 and 40.5; 16 x 32/8, L 500, R = 32 18.9
+// 22.2 and 22.6, R = 96 30.4 and 27.7; 1 x 64/8, L 16384, R = 64 29.1 and 39.7, R = 128 45.2 and 40.5; 16 x 32/8, L 500, R = 32 18.9
 // and 24.2, R = 40 32.6 and 24.4.
 int attn_q8_pick_kernel(const gsd_attn_params* p, int sm_count) {
     if (p->kernel != GSD_ATTN_AUTO) return p->kernel;
