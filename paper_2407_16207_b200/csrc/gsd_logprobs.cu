@@ -32,7 +32,7 @@ constexpr int kVecs = 8;                            // 16-byte loads of a thread
 constexpr int kCtasPerSm = 3;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kGroup = 1024;                        // sequences whose rows are shared out together
+constexpr int kGroup = 1024;                        // sequences whose rows are shared out together, at most
 
 struct SliceStats {
     float m, s, u, pad;
@@ -48,10 +48,11 @@ struct LogprobArgs {
     int32_t* status;
     int B, N, V, T, k;
     int loads, warps;               // of a row; of a group of sequences
+    int per_group;                  // sequences
     // Warp w has the loads from w * per_warp on, in the order of the rows, and its slice of row r the place r + w: from one
     // slice to the next either goes up by one.
     __device__ __forceinline__ long long per_warp(int rows) const { return ((long long)rows * loads + warps - 1) / warps; }
-    __device__ __forceinline__ size_t place0(int group) const { return (size_t)group * (warps + (size_t)min(kGroup, B) * T); }
+    __device__ __forceinline__ size_t place0(int group) const { return (size_t)group * (warps + (size_t)per_group * T); }
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) logprobs_scan_kernel(Log
     __shared__ float4 s_vec[TOP ? kWarps : 1][TOP ? kPool : 1];
     __shared__ int s_at[TOP ? kWarps : 1][TOP ? kPool : 1];
     __shared__ unsigned long long s_keys[TOP ? kWarps : 1][TOP ? kKeys : 1];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = blockIdx.y * kGroup, nb = min(kGroup, a.B - b0);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b0 = blockIdx.y * a.per_group, nb = min(a.per_group, a.B - b0);
     wait_for_predecessor();
     let_successor_start();
     rows_before(a, b0, nb, s_from);
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) logprobs_join_kernel(LogprobA
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.y;
     // (the inputs are older than the first launch, which let this one start after its own wait)
     const int len = min(max(a.lens[b], 0), a.T);
-    const int group = b / kGroup, b0 = group * kGroup, nb = min(kGroup, a.B - b0);
+    const int group = b / a.per_group, b0 = group * a.per_group, nb = min(a.per_group, a.B - b0);
     int from = 0, rows = 0;
     for (int k = lane; k < nb; k += 32) {
         const int n = min(max(a.lens[b0 + k], 0), a.T);
@@ -497,15 +498,20 @@ int loads_of(const gsd_logprobs_params* p) {
     const int n = (int)(((long long)p->V / 4 + 32 * kVecs - 1) / (32 * kVecs));
     return n > 0 ? n : 1;
 }
-// CTAs of a group of sequences.
-int blocks_of(const gsd_logprobs_params* p, int sm_count) {
-    const int groups = (p->B + kGroup - 1) / kGroup;
-    const long long most = (kCtasPerSm * sm_count + groups - 1) / groups, work = (long long)(p->B < kGroup ? p->B : kGroup) * p->T * loads_of(p);
-    return (int)(work < most ? work : most);
-}
-size_t places_of(const gsd_logprobs_params* p, int sm_count) {
-    const int groups = (p->B + kGroup - 1) / kGroup;
-    return (size_t)groups * ((size_t)blocks_of(p, sm_count) * kWarps + (size_t)(p->B < kGroup ? p->B : kGroup) * p->T);
+// Groups of as equal numbers of sequences as can be; the CTAs and the places in scratch of each.
+struct Groups {
+    int sequences, groups, blocks;
+    size_t places;
+};
+Groups groups_of(const gsd_logprobs_params* p, int sm_count) {
+    Groups g;
+    g.groups = (p->B + kGroup - 1) / kGroup;
+    g.sequences = (p->B + g.groups - 1) / g.groups;
+    g.groups = (p->B + g.sequences - 1) / g.sequences;
+    const long long most = (kCtasPerSm * sm_count + g.groups - 1) / g.groups, work = (long long)g.sequences * p->T * loads_of(p);
+    g.blocks = (int)(work < most ? work : most);
+    g.places = (size_t)g.groups * ((size_t)g.blocks * kWarps + (size_t)g.sequences * p->T);
+    return g;
 }
 }  // namespace
 }  // namespace gsd
@@ -514,7 +520,7 @@ extern "C" size_t gsd_token_logprobs_workspace_bytes(const gsd_logprobs_params* 
     using namespace gsd;
     DeviceInfo di;
     if (params_ok(p) != GSD_OK || device_info(&di) != 0) return 0;
-    return align_up(places_of(p, di.sm_count) * (sizeof(SliceStats) + 8 * (size_t)p->k), 256);
+    return align_up(groups_of(p, di.sm_count).places * (sizeof(SliceStats) + 8 * (size_t)p->k), 256);
 }
 
 extern "C" int gsd_token_logprobs(const float* logits, const int32_t* nodes, const int32_t* tokens, const int32_t* lens,
@@ -532,14 +538,14 @@ extern "C" int gsd_token_logprobs(const float* logits, const int32_t* nodes, con
     LogprobArgs a;
     a.logits = logits; a.nodes = nodes; a.tokens = tokens; a.lens = lens; a.logprobs = logprobs; a.entropy = entropy;
     a.top_tokens = top_tokens; a.top_logprobs = top_logprobs; a.status = status;
-    const int blocks = blocks_of(p, di.sm_count), groups = (p->B + kGroup - 1) / kGroup;
-    a.B = p->B; a.N = p->N; a.V = p->V; a.T = p->T; a.k = p->k; a.loads = loads_of(p); a.warps = blocks * kWarps;
-    const size_t places = places_of(p, di.sm_count);
+    const Groups g = groups_of(p, di.sm_count);
+    a.B = p->B; a.N = p->N; a.V = p->V; a.T = p->T; a.k = p->k; a.loads = loads_of(p); a.warps = g.blocks * kWarps; a.per_group = g.sequences;
+    const size_t places = g.places;
     if (!workspace || workspace_bytes < places * (sizeof(SliceStats) + 8 * (size_t)p->k)) return GSD_ERR_WORKSPACE;
     if (((uintptr_t)workspace & 7u) != 0) return GSD_ERR_MISALIGNED;
     a.stats = (SliceStats*)workspace;
     a.keys = (unsigned long long*)((char*)workspace + places * sizeof(SliceStats));
-    GSD_CUDA_TRY(launch_dependent(p->k > 0 ? logprobs_scan_kernel<true> : logprobs_scan_kernel<false>, dim3(blocks, groups), dim3(kThreads), 0, (cudaStream_t)stream, a));
+    GSD_CUDA_TRY(launch_dependent(p->k > 0 ? logprobs_scan_kernel<true> : logprobs_scan_kernel<false>, dim3(g.blocks, g.groups), dim3(kThreads), 0, (cudaStream_t)stream, a));
     const long long most = (16ll * di.sm_count + p->B - 1) / p->B, join = (p->T + kJoinWarps - 1) / kJoinWarps;
     GSD_CUDA_TRY(launch_dependent(p->k > 0 ? logprobs_join_kernel<true> : logprobs_join_kernel<false>, dim3((unsigned)(join < most ? join : most), p->B), dim3(kJoinWarps * 32), 0, (cudaStream_t)stream, a));
     return GSD_OK;
