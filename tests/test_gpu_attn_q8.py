@@ -122,6 +122,14 @@ def test_key_ranges(kernel, splits):
         check(x, call(x, num_splits=splits, kernel=kernel))
 
 
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("N,G", [(1, 17), (24, 1), (33, 1), (10, 4), (41, 1), (6, 8), (7, 7), (28, 2), (57, 1), (13, 5), (36, 2), (97, 1)])
+def test_row_groups_of_few_rows(N, G, D, splits):
+    x = make(11, 2, N, 2 * G, 2, D, 290, [289, 33], "int8" if N & 1 else "e4m3", 32)
+    check(x, call(x, kernel=1, num_splits=splits))
+
+
 @pytest.mark.parametrize("kernel", [1, 2])
 def test_rows_that_see_nothing_are_zero(kernel):
     x = make(4, 2, 11, 8, 2, 128, 64, [0, 40], "e4m3", 16, mask="none")
