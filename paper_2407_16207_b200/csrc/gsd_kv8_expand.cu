@@ -107,6 +107,8 @@ __global__ void __launch_bounds__(kThreads) kv8_expand_kernel(ExpandArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float v[4];
+                // (int8 through fp16 or bf16 arithmetic instead of a conversion per code: 1 x 64/8 heads, N 32, L 32768 76.8 us instead
+                // of 70.4, e4m3 by bf16 arithmetic the same)
                 if constexpr (INT8) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] = (float)(int8_t)(w[i] >> (8 * j));
