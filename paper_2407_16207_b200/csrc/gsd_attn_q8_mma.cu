@@ -403,10 +403,12 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
 
     // ---- draft tiles: bf16 rows straight from global memory, by bf16 products
     if (n_prefix * kWarps + first < t_end) {
-        // (the unit of the accumulators: weights 2^(kWeightBits - e_ref) must fit bf16)
-        if (e_ref < -100) {
-            const float back = two(max(e_ref + 100, -126));
-            e_ref = -100;
+        // (a unit near that of the draft rows, which are not scaled: in a smaller one, that of a warp without a prefix tile or with
+        // one of zeros, the products of large rows would be beyond fp32; what the accumulators hold by then loses nothing that
+        // is above 2^-126)
+        if (e_ref < 0) {
+            const float back = two(e_ref);
+            e_ref = 0;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
