@@ -450,10 +450,13 @@ typedef struct gsd_kv8_params {
  *   K_j = k_cache[b,j,c,:] * 2^k_exp[b, j / block, c], V_j likewise, for cache rows j < seq_lens[b];
  *   K_j, V_j = draft_k, draft_v[b,j,c,:] for draft rows j with bit j of ancestor_mask[b][n] set
  *   out[b,n,h,:] = sum_j softmax_j(scale * <q[b,n,h,:], K_j>) * V_j
- * On the way to the products only the softmax weights are rounded, to bf16 or finer (where a weight times the scale of its V
- * is below 2^-22 of the largest such product: to 2^-33 of that), and elements of q that lie more than 2^38 below the largest
- * of their row.  Sums and statistics are fp32, the output is bf16.  With N = 1 and a mask of one set bit it is ordinary
- * single-token decoding.  Everything else is as for gsd_verify_attn: literal mask bits, rows at positions >=
+ * On the way to the products only the softmax weights are rounded, to bf16 or finer, and elements of q that lie more than
+ * 2^38 below the largest of their row.  (The kernel for few rows rounds weights of cache rows to fp16 while the scales of V
+ * lie within 2^12 of one another: those below 2^-10 of the row's largest are then off by up to 2^-21 of that largest.
+ * It takes a V block with the exponent GSD_KV8_EXP_MIN for zeros beside blocks whose scale is more than 2^12 larger.)  Sums
+ * and statistics are fp32, and sums of weights times values, with weights of up to 2^8, have to stay within its range: values of
+ * V of up to 2^100 always do.  The output is bf16.  With N = 1 and a mask of one set bit it is ordinary single-token
+ * decoding.  Everything else is as for gsd_verify_attn: literal mask bits, rows at positions >=
  * seq_lens[b] never reach the result whatever their codes and exponents are, nor do draft rows that no node sees, and
  * a row with no visible key yields zeros.  Exponents outside [-117, 119] are not expected in visible blocks.
  *

@@ -7,7 +7,11 @@
 // four and eight significant bits): ek is one factor of a tile's scores, ev one of its weights, so nothing is
 // multiplied per cache element.  fp16 holds a query row exactly once a power of two has brought its maximum to 2^14
 // (what falls below 2^-24 then is under 2^-38 of the maximum), and a weight p 2^(8 + ev - e_ref) to 11 bits, e_ref the
-// largest ev met so far; the accumulators are in units of 2^(e_ref - 8).
+// largest ev met so far; the accumulators are in units of 2^(e_ref - 8).  That holds while the scales of V that a warp has
+// met lie within 2^12: what is below 2^-14 in fp16, p < 2^-10 at most, is then off by 2^-21 of the row's largest p.  A
+// scale that is further away, of a block that a row may give no weight, would take the bits of all others; from such a tile on
+// the accumulators are in units of 1 and weights p 2^ev and codes go to the product as bf16, which has the exponents of
+// fp32.  Blocks at the least exponent, as the writers give zeros, do not count for the distance.
 //
 // Every warp has tiles of 16 keys of its own, a ring of them in shared memory filled by asynchronous copies and nothing to
 // wait for but its own; the warps meet once, at the end.  What bounds it is instructions: 16 keys (4 KB) of eight rows
@@ -35,6 +39,7 @@ namespace {
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kKeys = 16;                    // keys of a warp's tile
 constexpr int kWeightBits = 8;               // what weights are brought up by in fp16
+constexpr int kSpread = 12;                  // log2 of how far the scales of V may lie apart for weights in fp16
 constexpr float kLag = 7.f;                  // the running maximum of a row may lag behind by this much (log2 units): weights stay below 2^15
 
 struct Q8Params {
@@ -107,6 +112,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
+}
+// Two fp16 values of up to eight significant bits as bf16.
+__device__ __forceinline__ uint32_t bf16_from_f16(uint32_t v) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+    return pack_bf16(f.x, f.y);
 }
 // 8x8 fp16 or bf16 values, a row a quarter of lanes -> their transpose.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
@@ -254,6 +264,9 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
         l_run[nt][0] = l_run[nt][1] = 0.f;
     }
     int e_ref = -126;                                                                    // accumulators: units of 2^(e_ref - kWeightBits)
+    int e_low = 127;                                                                     // the least scale of V met, GSD_KV8_EXP_MIN aside
+    bool apart = false;                                                                  // the scales are too far apart for fp16
+    auto back_from = [](int from, int to) { return from - to < -126 ? 0.f : two(from - to); };
 
     // Products s (times mult[.][.]: log2 units; hidden ones -inf) -> weights 2^(s - m + shift) in place.  The running maximum is
     // raised when a score exceeds it by more than kLag; the accumulators then follow, as they do a larger unit.
@@ -361,19 +374,17 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
                 }
         }
         float back = 1.f;
-        if (ev > e_ref) {
-            back = two(max(e_ref - ev, -126));                                           // (below 2^-126 of the unit: nothing is left)
-            e_ref = ev;
+        if (!apart && (ev > e_ref || (ev < e_low && ev > GSD_KV8_EXP_MIN))) {
+            if (ev > GSD_KV8_EXP_MIN) e_low = min(e_low, ev);
+            const int top = max(ev, e_ref);
+            apart = top - e_low > kSpread;
+            const int to = apart ? kWeightBits : top;
+            back = back_from(e_ref, to);
+            e_ref = to;
         }
-        // (a block far below the unit: its weights vanish in fp16 but still count in the sum)
-        const int shift = max(ev - e_ref + kWeightBits, -40);
+        // (zeros, far below the unit: their weights vanish in fp16 but still count in the sum)
+        const int shift = apart ? 0 : max(ev - e_ref + kWeightBits, -40);
         softmax(s, mult, back, (float)shift, two(-shift));
-        uint32_t pf[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            pf[nt][0] = transpose8(pack_f16(s[nt][0], s[nt][1]));
-            pf[nt][1] = transpose8(pack_f16(s[nt][2], s[nt][3]));
-        }
         // O^T += V^T P^T: the lane's keys are 2 j4, 2 j4 + 1, and these + 8; its columns (D / 8) i8 + 2 mt and the one behind
         uint32_t vw[4][D / 32];
 #pragma unroll
@@ -387,36 +398,58 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
                 vw[x][0] = v.x; vw[x][1] = v.y;
             }
         }
+        uint32_t pf[NT][2];
+        if (!apart) {
 #pragma unroll
-        for (int y = 0; y < D / 32; ++y)
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-                uint32_t a[4];
-                widen<INT8>(__byte_perm(vw[0][y], vw[1][y], z ? 0x7362 : 0x5140), a[0], a[1]);
-                widen<INT8>(__byte_perm(vw[2][y], vw[3][y], z ? 0x7362 : 0x5140), a[2], a[3]);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][y * 2 + z], a, pf[nt][0], pf[nt][1]);
+            for (int nt = 0; nt < NT; ++nt) {
+                pf[nt][0] = transpose8(pack_f16(s[nt][0], s[nt][1]));
+                pf[nt][1] = transpose8(pack_f16(s[nt][2], s[nt][3]));
             }
+#pragma unroll
+            for (int y = 0; y < D / 32; ++y)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    uint32_t a[4];
+                    widen<INT8>(__byte_perm(vw[0][y], vw[1][y], z ? 0x7362 : 0x5140), a[0], a[1]);
+                    widen<INT8>(__byte_perm(vw[2][y], vw[3][y], z ? 0x7362 : 0x5140), a[2], a[3]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][y * 2 + z], a, pf[nt][0], pf[nt][1]);
+                }
+        } else {
+            const float unit = two(ev);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                pf[nt][0] = transpose8(pack_bf16(s[nt][0] * unit, s[nt][1] * unit));
+                pf[nt][1] = transpose8(pack_bf16(s[nt][2] * unit, s[nt][3] * unit));
+            }
+#pragma unroll
+            for (int y = 0; y < D / 32; ++y)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    uint32_t a[4];
+                    widen<INT8>(__byte_perm(vw[0][y], vw[1][y], z ? 0x7362 : 0x5140), a[0], a[1]);
+                    widen<INT8>(__byte_perm(vw[2][y], vw[3][y], z ? 0x7362 : 0x5140), a[2], a[3]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) a[x] = bf16_from_f16(a[x]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][y * 2 + z], a, pf[nt][0], pf[nt][1]);
+                }
+        }
         __syncwarp();                       // the stage has been read: a copy may take its place
     }
     cp_async_wait<0>();
 
     // ---- draft tiles: bf16 rows straight from global memory, by bf16 products
     if (n_prefix * kWarps + first < t_end) {
-        // (a unit near that of the draft rows, which are not scaled: in a smaller one, that of a warp without a prefix tile or with
-        // one of zeros, the products of large rows would be beyond fp32; what the accumulators hold by then loses nothing that
-        // is above 2^-126)
-        if (e_ref < 0) {
-            const float back = two(e_ref);
-            e_ref = 0;
+        // in units of 1: the rows are not scaled, and weights have the exponents of fp32
+        const float back = back_from(e_ref, kWeightBits);
+        e_ref = kWeightBits;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int mt = 0; mt < MTL; ++mt)
+            for (int mt = 0; mt < MTL; ++mt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[nt][mt][e] *= back;
-        }
-        const float shift = (float)(kWeightBits - e_ref), unshift = two(max(e_ref - kWeightBits, -126));
+                for (int e = 0; e < 4; ++e) o[nt][mt][e] *= back;
         const __nv_bfloat16* dk = p.draft_k + ((size_t)b * N * p.Hkv + c) * D;
         const __nv_bfloat16* dv = p.draft_v + ((size_t)b * N * p.Hkv + c) * D;
 #pragma unroll 1
@@ -467,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
                 for (int e = 0; e < 4; ++e)
                     if (!((bits[nt][e & 1] >> (i8 + (e >> 1) * 8)) & 1u)) s[nt][e] = -CUDART_INF_F;
             }
-            softmax(s, mult, 1.f, shift, unshift);
+            softmax(s, mult, 1.f, 0.f, 1.f);
             uint32_t pf[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -496,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
     }
 
     // ---- the warps' results meet in the memory of the rings, each warp brings a share of the columns together
-    const float in_units = two(e_ref) * two(-kWeightBits);       // (below 2^-126: one product, exact)
+    const float in_units = back_from(e_ref, kWeightBits);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
