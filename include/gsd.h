@@ -455,7 +455,8 @@ typedef struct gsd_kv8_params {
  * lie within 2^12 of one another: those below 2^-10 of the row's largest are then off by up to 2^-21 of that largest.
  * It takes a V block with the exponent GSD_KV8_EXP_MIN for zeros beside blocks whose scale is more than 2^12 larger.)  Sums
  * and statistics are fp32, and sums of weights times values, with weights of up to 2^8, have to stay within its range: values of
- * V of up to 2^100 always do.  The output is bf16.  With N = 1 and a mask of one set bit it is ordinary single-token
+ * V of up to 2^100 always do.  Scores (scale * <q, K>) may be of any size that fp32 holds with few rows, and up to 2^29 in the
+ * tcgen05 kernel.  The output is bf16.  With N = 1 and a mask of one set bit it is ordinary single-token
  * decoding.  Everything else is as for gsd_verify_attn: literal mask bits, rows at positions >=
  * seq_lens[b] never reach the result whatever their codes and exponents are, nor do draft rows that no node sees, and
  * a row with no visible key yields zeros.  Exponents outside [-117, 119] are not expected in visible blocks.

@@ -108,6 +108,13 @@ __device__ __forceinline__ float fast_exp2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Pairs in place, an instruction for both.
+__device__ __forceinline__ void mul2(float& a0, float& a1, float b0, float b1) {
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}" : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1) {
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}" : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t d;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
@@ -268,21 +275,26 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
     bool apart = false;                                                                  // the scales are too far apart for fp16
     auto back_from = [](int from, int to) { return from - to < -126 ? 0.f : two(from - to); };
 
-    // Products s (times mult[.][.]: log2 units; hidden ones -inf) -> weights 2^(s - m + shift) in place.  The running maximum is
+    // Products s (times mult[.][.]: log2 units; hidden ones -inf) -> weights 2^(s - m) in place.  The running maximum is
     // raised when a score exceeds it by more than kLag; the accumulators then follow, as they do a larger unit.
-    auto softmax = [&](float (&s)[NT][4], const float (&mult)[NT][2], float unit_back, float shift, float unshift) {
+    // (The maximum is taken off rounded scores, not off the products in one step: the largest product differs from the maximum
+    // by what that was rounded by, 2^6 where scores are 2^30, and its weight was then beyond fp16.)
+    auto softmax = [&](float (&s)[NT][4], const float (&mult)[NT][2], float unit_back) {
         bool raise = unit_back != 1.f;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            mul2(s[nt][0], s[nt][1], mult[nt][0], mult[nt][1]);
+            mul2(s[nt][2], s[nt][3], mult[nt][0], mult[nt][1]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) raise |= fmaxf(s[nt][e], s[nt][e + 2]) * mult[nt][e] > m_run[nt][e] + kLag;
+            for (int e = 0; e < 2; ++e) raise |= fmaxf(s[nt][e], s[nt][e + 2]) - m_run[nt][e] > kLag;
+        }
         if (__any_sync(0xFFFFFFFFu, raise)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float a[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(s[nt][e], s[nt][e + 2]) * mult[nt][e];
+                    float mx = fmaxf(s[nt][e], s[nt][e + 2]);
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
                     const float m_new = fmaxf(m_run[nt][e], mx), m_use = m_new == -CUDART_INF_F ? 0.f : m_new;   // (nothing visible yet)
@@ -299,14 +311,17 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
             }
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            float off[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float off = shift - (m_run[nt][e] == -CUDART_INF_F ? 0.f : m_run[nt][e]);
-                s[nt][e] = fast_exp2(fmaf(s[nt][e], mult[nt][e], off));
-                s[nt][e + 2] = fast_exp2(fmaf(s[nt][e + 2], mult[nt][e], off));
-                l_run[nt][e] = fmaf(s[nt][e] + s[nt][e + 2], unshift, l_run[nt][e]);
-            }
+            for (int e = 0; e < 2; ++e) off[e] = m_run[nt][e] == -CUDART_INF_F ? 0.f : -m_run[nt][e];
+            add2(s[nt][0], s[nt][1], off[0], off[1]);
+            add2(s[nt][2], s[nt][3], off[0], off[1]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[nt][e] = fast_exp2(s[nt][e]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) l_run[nt][e] += s[nt][e] + s[nt][e + 2];
+        }
     };
 
     uint32_t stage = ring, fill = ring + (ST - 1) * (2 * T::TILE);
@@ -382,9 +397,14 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
             back = back_from(e_ref, to);
             e_ref = to;
         }
-        // (zeros, far below the unit: their weights vanish in fp16 but still count in the sum)
-        const int shift = apart ? 0 : max(ev - e_ref + kWeightBits, -40);
-        softmax(s, mult, back, (float)shift, two(-shift));
+        softmax(s, mult, back);
+        // (zeros far below the unit: their weights vanish in fp16)
+        const float unit = two(apart ? ev : max(ev - e_ref + kWeightBits, -40));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            mul2(s[nt][0], s[nt][1], unit, unit);
+            mul2(s[nt][2], s[nt][3], unit, unit);
+        }
         // O^T += V^T P^T: the lane's keys are 2 j4, 2 j4 + 1, and these + 8; its columns (D / 8) i8 + 2 mt and the one behind
         uint32_t vw[4][D / 32];
 #pragma unroll
@@ -416,11 +436,10 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
                     for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][y * 2 + z], a, pf[nt][0], pf[nt][1]);
                 }
         } else {
-            const float unit = two(ev);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                pf[nt][0] = transpose8(pack_bf16(s[nt][0] * unit, s[nt][1] * unit));
-                pf[nt][1] = transpose8(pack_bf16(s[nt][2] * unit, s[nt][3] * unit));
+                pf[nt][0] = transpose8(pack_bf16(s[nt][0], s[nt][1]));
+                pf[nt][1] = transpose8(pack_bf16(s[nt][2], s[nt][3]));
             }
 #pragma unroll
             for (int y = 0; y < D / 32; ++y)
@@ -500,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, Q8Geo<D, NT>::BLOCKS) attn_q8_mma_ke
                 for (int e = 0; e < 4; ++e)
                     if (!((bits[nt][e & 1] >> (i8 + (e >> 1) * 8)) & 1u)) s[nt][e] = -CUDART_INF_F;
             }
-            softmax(s, mult, 1.f, 0.f, 1.f);
+            softmax(s, mult, 1.f);
             uint32_t pf[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {

@@ -134,3 +134,21 @@ def test_an_infinity_in_the_cache_blanks_nothing_but_its_block(fmt, T):
     assert x["ve"][0, 1, 1] == 119
     for got in outs:
         check(x, got)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("D", [128, 64])
+def test_scores_beyond_any_rounding(D, fmt):
+    # few rows: the key that points with the query has the weight 1 exactly, whatever the size of its score, and what is
+    # not rounded stays: its value
+    for up in (10, 13, 14, 15, 16, 17, 18, 20, 26, 30, 40, 60):
+        x = make(27, 1, 1, 4, 2, D, 64, [34], fmt, 32, mask="none")
+        x["q"] = bf16(np.abs(x["q"].float().numpy()) * 2.0 ** up + 2.0 ** up)
+        x["k"][:] = constant(-33.0, fmt, 0)
+        x["k"][0, 5, 0] = x["k"][0, 33, 1] = constant(29.0, fmt, 0)
+        x["ke"][:] = 0
+        x["ve"][:] = -3
+        got = call(x, kernel=1).double().cpu().numpy()[0, 0]
+        v = np.ldexp(kv8_ref.values(x["v"][0], fmt), -3)
+        ref = np.stack([v[5, 0], v[5, 0], v[33, 1], v[33, 1]])
+        assert np.array_equal(got, ref), up
