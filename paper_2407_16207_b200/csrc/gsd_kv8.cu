@@ -13,10 +13,15 @@
 // 16-byte pieces a thread, holds the item in registers: one read of the rows, the maximum by shuffles and shared memory, one
 // write.  Heads follow one another, so that groups side by side read whole rows.  Bound by DRAM for prompts, by two
 // dependent trips to memory (length and path, then the rows) for accepted paths; those go to one cluster of CTAs per
-// sequence, which may advance seq_lens itself once every CTA of it has read the old length.
+// sequence, which may advance seq_lens itself once every CTA of it has read the old length.  Where the exponent of a block
+// grows, its earlier rows take another trip, or several: a group has room for kPieces pieces of each thread at a time.
 // Measured: 8 x 4096 tokens of 8 heads, e4m3: blocks of 16 38.1 us (80% of the copy rate), of 128 42.0 us, int8 40.2 and 44.5;
 // 8 paths of up to 17 tokens 4.6 us, 32 of up to 10 tokens of 40 heads 7.3 us.  3 to 64 CTAs an SM, 64 instead of 80
 // registers: the same within 3%, but 34 and 49 us for two of the appends with one wave of CTAs.
+// Paths behind blocks of 16, 64 and 128 tokens that hold all but one, no exponent growing and all of them (calls of a captured
+// graph, which add 0.5 to 1.2 us): the 8 paths 5.1, 6.4, 6.2 and 5.6, 8.7, 11.8 us, the 32 paths 9.8, 9.7, 10.1 and 14.0, 22.0, 35.3 us; one
+// row of 32 heads behind blocks of 128 4.1 and 12.8 us.  With the earlier rows read and written one piece after the other all
+// growing took 8.7, 21.8, 38.1; 22.0, 57.6, 105.5; and 45.3 us.
 #include "gsd_internal.cuh"
 #include "gsd_kv8.cuh"
 #include <initializer_list>
@@ -220,12 +225,19 @@ __global__ void __launch_bounds__(kThreads) kv8_write_kernel(WriteArgs a) {
                 *reinterpret_cast<uint2*>(dst + (size_t)pos * a.Hkv * D + at % ROW_PIECES * 8) = c;
             }
             if (held && e > e_old) {
-                // the earlier rows of the block in the new scale
+                // the earlier rows of the block in the new scale, eight 16-byte pieces of a thread on their way
                 const float g = e - e_old > 126 ? 0.f : two(e_old - e);
-                for (int at = t; at < (s.L - lo) * ROW_PIECES; at += group) {
-                    uint2* c = reinterpret_cast<uint2*>(dst + (size_t)(lo + at / ROW_PIECES) * a.Hkv * D + at % ROW_PIECES * 8);
-                    const uint2 w = *c;
-                    *c = make_uint2(rescale4<INT8>(w.x, g), rescale4<INT8>(w.y, g));
+                constexpr int PIECES = D / 16;
+                const int held_pieces = (s.L - lo) * PIECES;
+                for (int at0 = t; at0 < held_pieces; at0 += kPieces * group) {
+                    auto where = [&](int at) { return reinterpret_cast<uint4*>(dst + (size_t)(lo + at / PIECES) * a.Hkv * D + at % PIECES * 16); };
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k)
+                        if (at0 + k * group < held_pieces) x[k] = *where(at0 + k * group);
+#pragma unroll
+                    for (int k = 0; k < kPieces; ++k)
+                        if (at0 + k * group < held_pieces)
+                            *where(at0 + k * group) = make_uint4(rescale4<INT8>(x[k].x, g), rescale4<INT8>(x[k].y, g), rescale4<INT8>(x[k].z, g), rescale4<INT8>(x[k].w, g));
                 }
             }
             if (t == 0 && GSD_IN_BOUNDS(blk < a.NB, a.status)) *ex = (int8_t)e;
