@@ -152,3 +152,15 @@ def test_scores_beyond_any_rounding(D, fmt):
         v = np.ldexp(kv8_ref.values(x["v"][0], fmt), -3)
         ref = np.stack([v[5, 0], v[5, 0], v[33, 1], v[33, 1]])
         assert np.array_equal(got, ref), up
+
+
+@pytest.mark.parametrize("kernel", [0, 1, 2])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_chunks_of_a_prompt(fmt, kernel):
+    # a chain of as many nodes as there can be, over an empty cache and behind earlier chunks
+    for D, Hq, Hkv in ((128, 4, 2), (64, 2, 1)):
+        if kernel == 2 and D == 64:
+            continue
+        for N, lens in ((512, [0, 513]), (511, [130, 1])):
+            x = make(28, 2, N, Hq, Hkv, D, 520, lens, fmt, 64, mask="chain")
+            check(x, call(x, kernel=kernel))
