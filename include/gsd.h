@@ -424,7 +424,9 @@ int gsd_commit_kv(void* k_cache, void* v_cache, const void* draft_k, const void*
 
 /*
  * The 8-bit KV cache.  The paper keeps the committed prefix in a KV cache (Sec. 4.2) and does not say how it is
- * stored; held in 8 bits it takes half of the memory, and of the time that attention spends on reading it.
+ * stored; held in 8 bits it takes half of the memory.  Attention over it is faster than over a bf16 cache for single tokens;
+ * for draft graphs it takes 1.1 to 1.8 times as long, and with many stacked rows it needs scratch for the rows in bf16
+ * (gsd_verify_attn_q8).
  *
  *   codes      [B, Lmax, Hkv, D] bytes, K and V each: e4m3 (GSD_KV8_E4M3) or two's complement (GSD_KV8_INT8)
  *   exponents  [B, ceil(Lmax / block), Hkv] int8, K and V each: rows j of block j / block of a head share a scale
@@ -468,7 +470,11 @@ typedef struct gsd_kv8_params {
  *                     GSD_ATTN_SPLIT_PER_SEQUENCE are read as 0.  kernel: GSD_ATTN_AUTO, GSD_ATTN_MMA, or
  *                     GSD_ATTN_TCGEN05 (as for gsd_verify_attn, D == 128 and a group size that divides 128)
  *   c                 host
- *   workspace         gsd_verify_attn_q8_workspace_bytes(p, c) bytes, 256-byte aligned
+ *   workspace         gsd_verify_attn_q8_workspace_bytes(p, c) bytes, 256-byte aligned.  Where the tcgen05 kernel runs (D 64 or
+ *                     128, more than 64 stacked rows N * Hq/Hkv, or more than 32 and twice the (sequence, kv head) pairs above the
+ *                     number of SMs) it holds the visible rows in bf16: 4 * B * Lmax * Hkv * D bytes, twice the codes of the
+ *                     cache, whatever seq_lens is, beside the size of draft_v and of the partial results; elsewhere the
+ *                     partial results alone.  One workspace serves all layers of a stream.
  */
 size_t gsd_verify_attn_q8_workspace_bytes(const gsd_attn_params* p, const gsd_kv8_params* c);
 int gsd_verify_attn_q8(const void* q, const void* k_cache, const void* v_cache, const int8_t* k_exp, const int8_t* v_exp,

@@ -258,10 +258,10 @@ int attn_q8_params_ok(const gsd_attn_params* p, const gsd_kv8_params* c) {
 }
 
 // The few-row kernel reads the cache once for 32 rows, one CTA an SM beyond 16; the tcgen05 kernel pays for the widening of
-// every row first.  us, few-row and tcgen05, D 128: 8 x 64/8 heads, L 2048, R = 32 22.8 and 42.3, R = 64 (128 items) 30.1 and
-// 42.3, R = 96 56.7 and 43.4; 4 x 32 heads, L 1000, R = 32 23.2 and 38.7, R = 40 (256 items) 41.0 and 39.1; 1 x 32, L 2048, R = 64
-// 22.2 and 22.6, R = 96 30.4 and 27.7; 1 x 64/8, L 16384, R = 64 29.1 and 39.7, R = 128 45.2 and 40.5; 16 x 32/8, L 500, R = 32 18.9
-// and 24.2, R = 40 32.6 and 24.4.
+// every row first.  us, few-row and tcgen05, D 128: 8 x 64/8 heads, L 2048, R = 32 22.9 and 35.7, R = 64 (128 items) 30.6 and
+// 35.9, R = 96 56.8 and 37.6; 4 x 32 heads, L 1000, R = 32 23.4 and 32.0, R = 40 (256 items) 34.0 and 32.5; 1 x 32, L 2048, R = 64
+// 22.5 and 22.6, R = 96 30.6 and 23.8; 1 x 64/8, L 16384, R = 64 29.3 and 34.1, R = 128 46.0 and 35.4; 16 x 32/8, L 500, R = 32 18.9
+// and 20.2, R = 40 27.6 and 20.4.
 int attn_q8_pick_kernel(const gsd_attn_params* p, int sm_count) {
     if (p->kernel != GSD_ATTN_AUTO) return p->kernel;
     const int G = p->Hq / p->Hkv, R = p->N * G;
@@ -287,7 +287,7 @@ AttnPlan attn_q8_make_plan(const gsd_attn_params* p, int sm_count) {
         as.num_splits = std::max(p->num_splits, 0);
         return attn_make_plan(&as, sm_count);
     }
-    // Few stacked rows: items of 16 or 32 of them, key ranges for as many CTAs as the device holds.
+    // Few stacked rows: items of 8, 16, 24 or 32 of them, key ranges for as many CTAs as the device holds.
     AttnPlan pl = {};
     const int R = p->N * (p->Hq / p->Hkv);
     pl.kernel = GSD_ATTN_MMA;

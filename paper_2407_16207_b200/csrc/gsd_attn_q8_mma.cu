@@ -19,11 +19,13 @@
 // O^T = V^T P^T, with 16 keys or columns and 8 rows each, weights turned round by a movmatrix.  A tile's maximum is looked
 // at row by row only when a score exceeds the running one by more than 2^7.
 //
-// Measured (device time, inputs from DRAM): 32 x 64/8 heads, N 1, L 4096 48.0 us, 85% of the copy rate; 8 x 64/8, N 1, L 500-4000
-// 14.8 us (22.1 over a bf16 cache); 4 x 32/8 heads of 64, N 12, L 1000-4000 16.4 us.  With 32 rows the products bound it, 64 of
-// 16x8x16 a tile: 1 x 32 heads, N 64, L 2048 22.2 us.  48 rows as 24 and 24, not 32 and 16, two CTAs an SM there and
+// Measured (device time, inputs from DRAM): 32 x 64/8 heads, N 1, L 4096 47.9 us, 85% of the copy rate, int8 48.3; 8 x 64/8, N 1, L
+// 500-4000 14.9 us (22.1 over a bf16 cache); 4 x 32/8 heads of 64, N 12, L 1000-4000 16.6 us (15.4); 1 x 32 heads, N 64, L 2048 22.6 us
+// (14.9).  With half of the blocks 2^14 below the others, on the bf16 products, such calls take 0 to 6% more.  With 32 rows latency bounds it:
+// an instruction in 29% of the cycles of two warps a scheduler, the tensor pipe 21% busy, most of the waiting for instructions
+// to be fetched (the loop is unrolled over rows and columns) and for fixed latencies; with 24 rows of 64 43% and 18%.  48 rows as 24 and 24, not 32 and 16, two CTAs an SM there and
 // draft rows asked for ahead of time took the heads of 64 from 19.6 to 16.4 us; two CTAs with 32 rows spill (4 x 32/8 heads
-// of 64, N 8, L 4000: 21.6 instead of 17.3 us).
+// of 64, N 8, L 4000: 21.6 instead of 17.3 us, as both were then).
 //
 // A lane takes its operands from whole 16-byte pieces of a row: the order of the head dimension inside a product
 // is free (queries are loaded in the same order), and so is the order of the output columns.

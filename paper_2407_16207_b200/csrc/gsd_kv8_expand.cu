@@ -4,10 +4,11 @@
 //   out[b,j,c,:] = code[b,j,c,:] * 2^exp[b, j / block, c]   for j < seq_lens[b]: exact, bf16 holds every such value
 //
 // With many rows a key is used by many CTAs, and widening it once here (one read and two bytes written an element, at the
-// rate of DRAM or, for caches of up to some 40 MB, of the L2) costs less than widening it in every one of them: the tensor
+// rate of DRAM or, for caches of up to some 40 MB, of the L2; conversions take 65% of what their pipe has) costs less than widening it in every one of them: the tensor
 // cores take no 8-bit operand beside a 16-bit one, and inside the attention kernel the widening warps, beside softmax
 // warps that are almost always ready, get an instruction in every 10 to 20 cycles and add to the code that the instruction
-// cache has to hold.  8 x 64/8 heads, N 256, L 4096: 432 to 620 us with four forms of that.
+// cache has to hold.  8 x 64/8 heads, N 256, L 4096: 432 to 790 us with four forms of that, the bf16 kernel alone 223; smaller row
+// counts, whose softmax warps have more room, were not measured.
 //
 // A thread widens 16 codes at a time, four pieces on their way.  Blocks of their own copy the draft block's V with zeros for
 // rows that no node of the sequence sees: the attention kernel multiplies every row of a tile, with a weight of 0 where it
