@@ -66,6 +66,8 @@ typedef enum gsd_status {
 
 #define GSD_DEV_BAD_KV       0x800u /* gsd_commit_kv_q8, gsd_append_kv_q8: a row held an infinity (stored as the largest code) or a NaN (stored as zero) */
 
+#define GSD_DEV_BAD_PAGE     0x1000u /* a page table entry outside [0, num_pages) where a row was to be read or written; zeros were read, or the rows from there on dropped */
+
 #define GSD_MAX_NODES 512          /* largest supported N (draft nodes per sequence) */
 
 /* kernel selection for gsd_verify_attn */
@@ -520,6 +522,132 @@ typedef struct gsd_append_params {
 int gsd_append_kv_q8(void* k_cache, void* v_cache, int8_t* k_exp, int8_t* v_exp, const void* k, const void* v,
                      const int32_t* counts, int32_t* seq_lens, const gsd_append_params* p, const gsd_kv8_params* c,
                      int32_t* status, void* stream);
+
+/*
+ * The paged KV cache.  The paper keeps the committed prefix in a KV cache (Sec. 4.2) and does not say where its rows lie;
+ * with a padded range of rows for every sequence a server holds memory for the longest context that each may reach.  Here the
+ * rows lie in pages of a common pool, and a table says which page holds which rows of a sequence:
+ *
+ *   k_pages, v_pages  [num_pages, page, Hkv, D] bf16
+ *   page_table        [B, max_pages] int32; row j of sequence b is row j % page of page page_table[b][j / page]
+ *
+ * `page` is 16, 32, 64, 128 or 256 rows; any number of pages the memory holds.  Several sequences may read the same pages (a
+ * common system prompt); a page that a call writes must not be named twice in what it reads or writes.  Only the entries that
+ * hold a visible row or get a new one are read, the rest of the table may be anything.  An entry outside [0, num_pages) among
+ * those never leads to an access: gsd_verify_attn_paged takes its rows for zeros, the writers drop the rows from the first
+ * without a page on, and GSD_DEV_BAD_PAGE says so.
+ */
+typedef struct gsd_page_params {
+    int32_t page;        /* rows of a page: 16, 32, 64, 128 or 256 */
+    int32_t num_pages;   /* pages of the pool, >= 1 */
+    int32_t max_pages;   /* row length of page_table, >= 1 */
+} gsd_page_params;
+
+/*
+ * gsd_verify_attn_paged - gsd_verify_attn over a paged cache (tree attention, Sec. 4.1; KV cache, Sec. 4.2).
+ *
+ *   q, draft_k, draft_v, ancestor_mask, seq_lens, out, workspace, status, stream   as for gsd_verify_attn
+ *   k_pages, v_pages, page_table   device in; the pages 16-byte aligned
+ *   p                 host; Lmax is the length that no sequence exceeds, at most max_pages * page and 2^30: the work is planned for it
+ *                     (the room in the table will do; a smaller bound makes better plans).  num_splits is 0 (choose) or the
+ *                     number of key ranges; GSD_ATTN_SPLIT_BALANCED and GSD_ATTN_SPLIT_PER_SEQUENCE are read as 0.  kernel:
+ *                     GSD_ATTN_AUTO, GSD_ATTN_MMA, or GSD_ATTN_TCGEN05 (D == 128 and a group size that divides 128)
+ *   c                 host
+ * With N = 1 and a mask of one set bit it is ordinary single-token decoding.  Rows at positions >= seq_lens[b] never reach
+ * the result whatever the pages hold there, and a row with no visible key yields zeros.
+ */
+size_t gsd_verify_attn_paged_workspace_bytes(const gsd_attn_params* p, const gsd_page_params* c);
+int gsd_verify_attn_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                          const void* draft_k, const void* draft_v, const uint32_t* ancestor_mask, const int32_t* seq_lens,
+                          void* out, const gsd_attn_params* p, const gsd_page_params* c, void* workspace,
+                          size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * gsd_commit_kv_paged - gsd_commit_kv into a paged cache: the draft K/V rows of the accepted path are copied to the places
+ * seq_lens[b], seq_lens[b] + 1, ... of the sequence, and seq_lens[b] is advanced by the rows written (cache update, Sec. 7.1 /
+ * Table 3).  Rows that would land at or past p->Lmax (at most max_pages * page and 2^30) are dropped (GSD_DEV_CACHE_FULL), as are the rows
+ * from the first on whose page the table does not name (GSD_DEV_BAD_PAGE).  Everything else is as for gsd_commit_kv; D is 64
+ * or 128, B at most 65535.
+ */
+int gsd_commit_kv_paged(void* k_pages, void* v_pages, const int32_t* page_table, const void* draft_k, const void* draft_v,
+                        const int32_t* accepted_nodes, const int32_t* accepted_len, int32_t* seq_lens,
+                        const gsd_commit_params* p, const gsd_page_params* c, int32_t* status, void* stream);
+
+/*
+ * Rotary positions.  The attention calls take Q and K with the positions applied; gsd_rotary applies them to the draft nodes'
+ * rows and gsd_append_kv_paged to the rows of a prompt on their way into the cache.  Of the D columns of a head the first
+ * 2 * pairs are rotated, pair i by
+ *
+ *   angle_i = (positions[axis[i]][b][t] + offsets[b]) * freqs[i]        (x, y) -> (x cos - y sin, x sin + y cos)
+ *
+ * With one axis that is the position in a text; with three (time, height, width) each pair follows one of them, in blocks or in
+ * turns as `axis` says.  The angle is formed and reduced in 64 bits, so that far positions lose nothing; sine, cosine and the
+ * rotation are fp32, and the result is rounded to bf16 once.  The columns behind are copied.
+ */
+#define GSD_ROTARY_HALVES 0       /* pair i: columns i and pairs + i */
+#define GSD_ROTARY_NEIGHBOURS 1   /* pair i: columns 2 i and 2 i + 1 */
+#define GSD_ROTARY_MAX_AXES 4
+typedef struct gsd_rotation {
+    int32_t pairs;       /* pairs of columns, a multiple of 8, 8 .. D / 2 */
+    int32_t layout;      /* GSD_ROTARY_HALVES or GSD_ROTARY_NEIGHBOURS */
+    int32_t axes;        /* position axes, 1 .. GSD_ROTARY_MAX_AXES */
+    uint8_t axis[64];    /* axis of each pair, below `axes`; entries from `pairs` on are not read */
+} gsd_rotation;
+
+/*
+ * gsd_rotary - rotary positions of the draft nodes' (or any tokens') Q and K rows.
+ *
+ *   q         [B, T, Hq, D] bf16 device in; the rows of a token (Hq * D elements) are contiguous, those of token b * T + t start
+ *             at (b * T + t) * q_stride elements, so that a slice of a fused projection's output can be passed as it is
+ *   k         [B, T, Hkv, D] bf16 device in, likewise with k_stride; NULL: q only
+ *   freqs     [pairs] fp32 device in: angle per position, in radians
+ *   positions [axes, B, T] int32 device in
+ *   offsets   [B] int32 device in or NULL: added to every position of the sequence (seq_lens, with the depth of a node as its
+ *             position)
+ *   q_out     [B, T, Hq, D], k_out [B, T, Hkv, D] bf16 device out, dense; may be q and k themselves if those are dense, must not
+ *             overlap them otherwise.  k_out is NULL with k
+ *   p, r      host
+ * Bases of q, k, q_out, k_out 16-byte aligned, strides multiples of 8 elements.  No workspace, no allocation, asynchronous on
+ * `stream`.
+ */
+typedef struct gsd_rotary_params {
+    int32_t B, T;        /* sequences, tokens of each */
+    int32_t Hq, Hkv;     /* heads of q and of k; Hkv is not read if k is NULL */
+    int32_t D;           /* head dimension: 64 or 128 */
+    int64_t q_stride;    /* elements from a token to the next in q, >= Hq * D */
+    int64_t k_stride;    /* the same in k, >= Hkv * D */
+} gsd_rotary_params;
+int gsd_rotary(const void* q, const void* k, const float* freqs, const int32_t* positions, const int32_t* offsets,
+               void* q_out, void* k_out, const gsd_rotary_params* p, const gsd_rotation* r, void* stream);
+
+/*
+ * gsd_append_kv_paged - the rows of a prompt, or of the next chunk of one, into a paged cache: k[b][0..counts[b]), rotated by
+ * position, and v[b][0..counts[b]) go to the places seq_lens[b], seq_lens[b] + 1, ... of the sequence, and seq_lens[b] is
+ * advanced by the rows written.  Rows that would land at or past p->Lmax (at most max_pages * page) are dropped
+ * (GSD_DEV_CACHE_FULL), as are the rows from the first on whose page the table does not name (GSD_DEV_BAD_PAGE); a count outside
+ * [0, T] is clamped (GSD_DEV_BAD_SEQ_LEN).
+ *
+ *   k_pages, v_pages  device in/out;  page_table device in
+ *   k, v      [B, T, Hkv, D] bf16 device in, token rows k_stride and v_stride elements apart as for gsd_rotary
+ *   counts    [B] int32 device in;  seq_lens [B] int32 device in/out
+ *   freqs, positions, offsets, r   the rotation of K, as for gsd_rotary.  positions NULL: the token's place in the sequence,
+ *             seq_lens[b] + t, on every axis (plus offsets[b], if given).  r and freqs NULL: K is copied like V
+ * offsets may be seq_lens itself (its old values count).  Tensor bases 16-byte aligned, strides multiples of 8 elements.  No
+ * workspace, no allocation, asynchronous on `stream`.
+ */
+typedef struct gsd_append_paged_params {
+    int32_t B;           /* sequences, at most 65535 */
+    int32_t T;           /* rows per sequence in k / v */
+    int32_t Hkv;         /* key/value heads */
+    int32_t D;           /* head dimension: 64 or 128 */
+    int32_t Lmax;        /* the length that no sequence may exceed, at most max_pages * page and 2^30 */
+    int64_t k_stride;    /* elements from a token to the next in k, >= Hkv * D */
+    int64_t v_stride;    /* the same in v */
+} gsd_append_paged_params;
+int gsd_append_kv_paged(void* k_pages, void* v_pages, const int32_t* page_table, const void* k, const void* v,
+                        const int32_t* counts, int32_t* seq_lens, const float* freqs, const int32_t* positions,
+                        const int32_t* offsets, const gsd_append_paged_params* p, const gsd_page_params* c,
+                        const gsd_rotation* r, int32_t* status, void* stream);
 
 /*
  * gsd_token_logprobs - what a server returns beside the tokens that a step emitted: the log probability of each under

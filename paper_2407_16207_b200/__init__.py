@@ -10,7 +10,8 @@ from .binding import (GSD_ATTN_AUTO, GSD_ATTN_MMA, GSD_ATTN_SPLIT_BALANCED, GSD_
                       gsd_verify_step_host_arena_bytes, gsd_version, gsd_debug_attn_wait, lib, library_path,
                       GSD_KV8_E4M3, GSD_KV8_EXP_MAX, GSD_KV8_EXP_MIN, GSD_KV8_INT8, gsd_append_kv_q8, gsd_commit_kv_q8,
                       gsd_token_logprobs, gsd_token_logprobs_workspace_bytes, gsd_verify_attn_q8,
-                      gsd_verify_attn_q8_workspace_bytes)
+                      gsd_verify_attn_q8_workspace_bytes, GSD_ROTARY_HALVES, GSD_ROTARY_NEIGHBOURS, gsd_append_kv_paged,
+                      gsd_commit_kv_paged, gsd_rotary, gsd_verify_attn_paged, gsd_verify_attn_paged_workspace_bytes)
 
 __all__ = ["GSD_ATTN_AUTO", "GSD_ATTN_MMA", "GSD_ATTN_SPLIT_BALANCED", "GSD_ATTN_SPLIT_PER_SEQUENCE", "GSD_ATTN_TCGEN05", "GsdError", "gsd_accept", "gsd_accept_sampled", "gsd_accept_sampled_workspace_bytes", "gsd_accept_static", "gsd_build_mask", "gsd_unmerge_tree", "gsd_draft_expand", "gsd_commit_kv",
            "gsd_accept_workspace_bytes", "gsd_verify_attn", "gsd_verify_attn_num_splits",
@@ -18,4 +19,5 @@ __all__ = ["GSD_ATTN_AUTO", "GSD_ATTN_MMA", "GSD_ATTN_SPLIT_BALANCED", "GSD_ATTN
            "gsd_verify_step_host_arena_bytes", "gsd_version", "gsd_debug_attn_wait", "lib", "library_path",
            "GSD_KV8_E4M3", "GSD_KV8_EXP_MAX", "GSD_KV8_EXP_MIN", "GSD_KV8_INT8", "gsd_append_kv_q8", "gsd_commit_kv_q8",
            "gsd_token_logprobs", "gsd_token_logprobs_workspace_bytes", "gsd_verify_attn_q8",
-           "gsd_verify_attn_q8_workspace_bytes"]
+           "gsd_verify_attn_q8_workspace_bytes", "GSD_ROTARY_HALVES", "GSD_ROTARY_NEIGHBOURS", "gsd_append_kv_paged",
+           "gsd_commit_kv_paged", "gsd_rotary", "gsd_verify_attn_paged", "gsd_verify_attn_paged_workspace_bytes"]

@@ -11,13 +11,15 @@ from __future__ import annotations
 import ctypes
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
 GSD_ATTN_AUTO, GSD_ATTN_MMA, GSD_ATTN_TCGEN05 = 0, 1, 2
 GSD_ATTN_SPLIT_BALANCED = -1      # num_splits: equal shares of key tiles per CTA, dealt out on the device
 GSD_ATTN_SPLIT_PER_SEQUENCE = -2  # num_splits: a split count per sequence, chosen on the device
+
+GSD_ROTARY_HALVES, GSD_ROTARY_NEIGHBOURS = 0, 1
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libgsd.so")
@@ -64,6 +66,24 @@ class AppendParams(ctypes.Structure):
                 ("Lmax", ctypes.c_int32)]
 
 
+class PageParams(ctypes.Structure):
+    _fields_ = [("page", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class Rotation(ctypes.Structure):
+    _fields_ = [("pairs", ctypes.c_int32), ("layout", ctypes.c_int32), ("axes", ctypes.c_int32), ("axis", ctypes.c_uint8 * 64)]
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64)]
+
+
+class AppendPagedParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("Lmax", ctypes.c_int32), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
 class LogprobsParams(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("V", ctypes.c_int32), ("T", ctypes.c_int32),
                 ("k", ctypes.c_int32)]
@@ -75,7 +95,9 @@ EXPORTS = ["gsd_version", "gsd_status_string", "gsd_last_cuda_error", "gsd_debug
            "gsd_accept_sampled_workspace_bytes", "gsd_draft_expand", "gsd_draft_expand_workspace_bytes",
            "gsd_commit_kv", "gsd_build_mask", "gsd_unmerge_tree", "gsd_verify_step_host",
            "gsd_verify_step_host_arena_bytes", "gsd_verify_attn_q8", "gsd_verify_attn_q8_workspace_bytes",
-           "gsd_commit_kv_q8", "gsd_append_kv_q8", "gsd_token_logprobs", "gsd_token_logprobs_workspace_bytes"]
+           "gsd_commit_kv_q8", "gsd_append_kv_q8", "gsd_token_logprobs", "gsd_token_logprobs_workspace_bytes",
+           "gsd_verify_attn_paged", "gsd_verify_attn_paged_workspace_bytes", "gsd_commit_kv_paged", "gsd_append_kv_paged",
+           "gsd_rotary"]
 
 
 def library_path() -> str:
@@ -142,6 +164,17 @@ def lib() -> ctypes.CDLL:
         L.gsd_token_logprobs.argtypes = [vp] * 8 + [ctypes.POINTER(LogprobsParams), vp, sz, vp, vp]
         L.gsd_token_logprobs_workspace_bytes.restype = sz
         L.gsd_token_logprobs_workspace_bytes.argtypes = [ctypes.POINTER(LogprobsParams)]
+        page, rot = ctypes.POINTER(PageParams), ctypes.POINTER(Rotation)
+        L.gsd_verify_attn_paged.restype = i32
+        L.gsd_verify_attn_paged.argtypes = [vp] * 9 + [ctypes.POINTER(AttnParams), page, vp, sz, vp, vp]
+        L.gsd_verify_attn_paged_workspace_bytes.restype = sz
+        L.gsd_verify_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(AttnParams), page]
+        L.gsd_commit_kv_paged.restype = i32
+        L.gsd_commit_kv_paged.argtypes = [vp] * 8 + [ctypes.POINTER(CommitParams), page, vp, vp]
+        L.gsd_append_kv_paged.restype = i32
+        L.gsd_append_kv_paged.argtypes = [vp] * 10 + [ctypes.POINTER(AppendPagedParams), page, rot, vp, vp]
+        L.gsd_rotary.restype = i32
+        L.gsd_rotary.argtypes = [vp] * 7 + [ctypes.POINTER(RotaryParams), rot, vp]
         _lib = L
     return _lib
 
@@ -151,7 +184,8 @@ _NATIVE_CALLS = ("gsd_verify_attn", "gsd_verify_attn_workspace_bytes", "gsd_acce
                  "gsd_accept_sampled", "gsd_accept_sampled_workspace_bytes", "gsd_binding_draft_expand",
                  "gsd_draft_expand_workspace_bytes", "gsd_build_mask", "gsd_commit_kv", "gsd_verify_attn_q8",
                  "gsd_verify_attn_q8_workspace_bytes", "gsd_commit_kv_q8", "gsd_append_kv_q8", "gsd_token_logprobs",
-                 "gsd_token_logprobs_workspace_bytes")
+                 "gsd_token_logprobs_workspace_bytes", "gsd_verify_attn_paged", "gsd_verify_attn_paged_workspace_bytes",
+                 "gsd_commit_kv_paged", "gsd_append_kv_paged", "gsd_rotary")
 _native = None
 _native_lib: Optional[ctypes.CDLL] = None      # the library the extension is bound to
 
@@ -675,6 +709,210 @@ def gsd_append_kv_q8(k_cache, v_cache, k_exp, v_exp, k, v, counts, seq_lens, *, 
         _check(lib().gsd_append_kv_q8(k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(),
                                       k.data_ptr(), v.data_ptr(), counts.data_ptr(), seq_lens.data_ptr(), ctypes.byref(p),
                                       ctypes.byref(c), _ptr(status), _stream(k_cache)))
+
+
+_PAGED_LMAX = 1 << 30
+
+
+def _check_pages(k_pages, v_pages, page_table, B) -> PageParams:
+    """The paged cache: pools [num_pages,page,Hkv,D] bf16 and a table [B,max_pages] int32."""
+    if k_pages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k_pages must be [num_pages,page,Hkv,D] and page_table [B,max_pages]")
+    P, page, Hkv, D = k_pages.shape
+    if page not in (16, 32, 64, 128, 256):
+        raise ValueError(f"pages must have 16, 32, 64, 128 or 256 rows, got {page}")
+    _want(k_pages, torch.bfloat16, (P, page, Hkv, D), "k_pages", True)
+    _want(v_pages, torch.bfloat16, (P, page, Hkv, D), "v_pages", True)
+    _want(page_table, torch.int32, (B, page_table.shape[1]), "page_table", True)
+    return PageParams(page, P, page_table.shape[1])
+
+
+def _paged_lmax(c: PageParams) -> int:
+    return min(c.max_pages * c.page, _PAGED_LMAX)
+
+
+def gsd_verify_attn_paged_workspace_bytes(B, N, Hq, Hkv, D, page, max_pages, *, max_len=0, num_splits=0, kernel=GSD_ATTN_AUTO) -> int:
+    c = PageParams(page, 1, max_pages)
+    p = AttnParams(B, N, Hq, Hkv, D, int(max_len) or _paged_lmax(c), 0.0, num_splits, kernel)
+    return int(lib().gsd_verify_attn_paged_workspace_bytes(ctypes.byref(p), ctypes.byref(c)))
+
+
+def gsd_verify_attn_paged(q, k_pages, v_pages, page_table, draft_k, draft_v, ancestor_mask, seq_lens,
+                          out: Optional[torch.Tensor] = None, *, max_len: int = 0, softmax_scale: float = 0.0,
+                          num_splits: int = 0, kernel: int = GSD_ATTN_AUTO, workspace: Optional[torch.Tensor] = None,
+                          status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """gsd_verify_attn over a cache in pages: pools k_pages / v_pages [num_pages,page,Hkv,D], page_table [B,max_pages] int32;
+    `max_len` is a length no sequence exceeds (0: the room in the table).  See gsd_verify_attn_paged in include/gsd.h.
+    Enqueued on the current stream; returns `out` [B,N,Hq,D] bf16."""
+    fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+    r = fast.verify_attn_paged(q, k_pages, v_pages, page_table, draft_k, draft_v, ancestor_mask, seq_lens, out, max_len,
+                               softmax_scale, num_splits, kernel, workspace, status)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r)
+        return r
+    if q.dim() != 4:
+        raise ValueError("q must be [B,N,Hq,D]")
+    bf = torch.bfloat16
+    B, N, Hq, D = q.shape
+    c = _check_pages(k_pages, v_pages, page_table, B)
+    Hkv = k_pages.shape[2]
+    _want(q, bf, (B, N, Hq, D), "q", True)
+    _want(k_pages, bf, (c.num_pages, c.page, Hkv, D), "k_pages", True)
+    _want(draft_k, bf, (B, N, Hkv, D), "draft_k", True)
+    _want(draft_v, bf, (B, N, Hkv, D), "draft_v", True)
+    if ancestor_mask.dtype not in (torch.int32, torch.uint32):
+        raise ValueError("ancestor_mask must hold 32-bit words (int32 or uint32)")
+    _want(ancestor_mask, ancestor_mask.dtype, (B, N, (N + 31) // 32), "ancestor_mask", True)
+    _want(seq_lens, torch.int32, (B,), "seq_lens", True)
+    _same_device(q, k_pages, v_pages, page_table, draft_k, draft_v, ancestor_mask, seq_lens, out, workspace, status)
+    if out is None:
+        out = torch.empty_like(q)
+    _want(out, bf, q.shape, "out", True)
+    p = AttnParams(B, N, Hq, Hkv, D, int(max_len) or _paged_lmax(c), float(softmax_scale), int(num_splits), int(kernel))
+    L = lib()
+    with torch.cuda.device(q.device):
+        need = int(L.gsd_verify_attn_paged_workspace_bytes(ctypes.byref(p), ctypes.byref(c)))
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        _check(L.gsd_verify_attn_paged(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+                                       draft_k.data_ptr(), draft_v.data_ptr(), ancestor_mask.data_ptr(), seq_lens.data_ptr(),
+                                       out.data_ptr(), ctypes.byref(p), ctypes.byref(c), _ptr(workspace), ws_bytes,
+                                       _ptr(status), _stream(q)))
+    return out
+
+
+def gsd_commit_kv_paged(k_pages, v_pages, page_table, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, *,
+                        status: Optional[torch.Tensor] = None) -> None:
+    """Copy the draft K/V rows of the accepted path behind the sequences' ends in a paged cache and advance seq_lens; see
+    gsd_commit_kv_paged in include/gsd.h.  Enqueued on the current stream."""
+    fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+    r = fast.commit_kv_paged(k_pages, v_pages, page_table, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, status)
+    if r is not None:
+        return _check(r)
+    if draft_k.dim() != 4 or accepted_nodes.dim() != 2:
+        raise ValueError("draft_k must be [B,N,Hkv,D] and accepted_nodes [B,Tcap]")
+    B, N, Hkv, D = draft_k.shape
+    c = _check_pages(k_pages, v_pages, page_table, B)
+    Tcap = accepted_nodes.shape[1]
+    _want(k_pages, torch.bfloat16, (c.num_pages, c.page, Hkv, D), "k_pages", True)
+    _want(draft_k, torch.bfloat16, (B, N, Hkv, D), "draft_k", True)
+    _want(draft_v, torch.bfloat16, (B, N, Hkv, D), "draft_v", True)
+    _want(accepted_nodes, torch.int32, (B, Tcap), "accepted_nodes", True)
+    _want(accepted_len, torch.int32, (B,), "accepted_len", True)
+    _want(seq_lens, torch.int32, (B,), "seq_lens", True)
+    _same_device(k_pages, v_pages, page_table, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, status)
+    p = CommitParams(B, N, Hkv, D, _paged_lmax(c), Tcap)
+    with torch.cuda.device(k_pages.device):
+        _check(lib().gsd_commit_kv_paged(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), draft_k.data_ptr(),
+                                         draft_v.data_ptr(), accepted_nodes.data_ptr(), accepted_len.data_ptr(),
+                                         seq_lens.data_ptr(), ctypes.byref(p), ctypes.byref(c), _ptr(status), _stream(k_pages)))
+
+
+def _token_stride(x: torch.Tensor, name: str) -> int:
+    """Elements from a token's rows to the next token's in x [B,T,H,D] bf16, whose rows of a token are contiguous."""
+    if x.dim() != 4 or x.dtype != torch.bfloat16:
+        raise ValueError(f"{name}: expected bfloat16 [B,T,H,D], got {x.dtype} {tuple(x.shape)}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    B, T, H, D = x.shape
+    s = x.stride(1) if T > 1 else x.stride(0) if B > 1 else H * D
+    if (x.stride(3) != 1 and D > 1) or (H > 1 and x.stride(2) != D) or (B > 1 and x.stride(0) != T * s):
+        raise ValueError(f"{name}: the rows of a token must be contiguous and the tokens a fixed distance apart, got strides "
+                         f"{tuple(x.stride())} for {tuple(x.shape)}")
+    return s
+
+
+def _rotation(freqs, positions, offsets, axes, pairs, B, T) -> Rotation:
+    if freqs.dim() != 1:
+        raise ValueError("freqs must be [pairs]")
+    n = freqs.shape[0]
+    _want(freqs, torch.float32, (n,), "freqs", True)
+    if positions is not None:
+        if positions.dim() != 3:
+            raise ValueError("positions must be [axes,B,T]")
+        _want(positions, torch.int32, (positions.shape[0], B, T), "positions", True)
+    if offsets is not None:
+        _want(offsets, torch.int32, (B,), "offsets", True)
+    axes = [0] * n if axes is None else [int(a) for a in axes]
+    count = positions.shape[0] if positions is not None else max(axes, default=0) + 1
+    if len(axes) != n or any(a < 0 or a >= count for a in axes):
+        raise ValueError(f"axes: expected an axis below {count} for each of {n} pairs")
+    return Rotation(n, GSD_ROTARY_NEIGHBOURS if pairs else GSD_ROTARY_HALVES, count, (ctypes.c_uint8 * 64)(*axes[:64]))
+
+
+def gsd_append_kv_paged(k_pages, v_pages, page_table, k, v, counts, seq_lens, *, freqs: Optional[torch.Tensor] = None,
+                        positions: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                        axes: Optional[Sequence[int]] = None, pairs: bool = False,
+                        status: Optional[torch.Tensor] = None) -> None:
+    """Write the first counts[b] rows of k / v [B,T,Hkv,D] behind the sequences' ends in a paged cache, K rotated by position on
+    the way if `freqs` is given (positions [axes,B,T]; None: the place in the sequence), and advance seq_lens; see
+    gsd_append_kv_paged in include/gsd.h and gsd_rotary.  k and v may be slices of a projection's output.  Enqueued on the
+    current stream."""
+    fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+    r = fast.append_kv_paged(k_pages, v_pages, page_table, k, v, counts, seq_lens, freqs, positions, offsets, axes, pairs, status)
+    if r is not None:
+        return _check(r)
+    ks, vs = _token_stride(k, "k"), _token_stride(v, "v")
+    B, T, Hkv, D = k.shape
+    if v.shape != k.shape:
+        raise ValueError(f"v: expected {tuple(k.shape)}, got {tuple(v.shape)}")
+    c = _check_pages(k_pages, v_pages, page_table, B)
+    _want(k_pages, torch.bfloat16, (c.num_pages, c.page, Hkv, D), "k_pages", True)
+    _want(counts, torch.int32, (B,), "counts", True)
+    _want(seq_lens, torch.int32, (B,), "seq_lens", True)
+    if freqs is None and not (positions is None and offsets is None and axes is None):
+        raise ValueError("positions, offsets and axes need freqs")
+    rot = None if freqs is None else _rotation(freqs, positions, offsets, axes, pairs, B, T)
+    _same_device(k_pages, v_pages, page_table, k, v, counts, seq_lens, freqs, positions, offsets, status)
+    p = AppendPagedParams(B, T, Hkv, D, _paged_lmax(c), ks, vs)
+    with torch.cuda.device(k_pages.device):
+        _check(lib().gsd_append_kv_paged(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), k.data_ptr(),
+                                         v.data_ptr(), counts.data_ptr(), seq_lens.data_ptr(), _ptr(freqs), _ptr(positions),
+                                         _ptr(offsets), ctypes.byref(p), ctypes.byref(c),
+                                         None if rot is None else ctypes.byref(rot), _ptr(status), _stream(k_pages)))
+
+
+def gsd_rotary(q, k, freqs, positions, *, offsets: Optional[torch.Tensor] = None, axes: Optional[Sequence[int]] = None,
+               pairs: bool = False, out: Optional[Tuple[torch.Tensor, Optional[torch.Tensor]]] = None
+               ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Rotary positions of q [B,T,Hq,D] and k [B,T,Hkv,D] (or None): pair i of the first 2 * len(freqs) columns turns by
+    (positions[axes[i],b,t] + offsets[b]) * freqs[i].  `axes` names the position axis of each pair (None: the first), `pairs`
+    says that neighbouring columns form a pair, else column i and i + len(freqs) do.  q and k may be slices of a projection's
+    output.  Returns new dense tensors, or `out`, which may be (q, k) themselves if those are dense.  See gsd_rotary in
+    include/gsd.h.  Enqueued on the current stream."""
+    fast = _native if _lib is not None and _lib is _native_lib else _marshal()
+    r = fast.rotary(q, k, freqs, positions, offsets, axes, pairs, out)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r)
+        return r
+    qs = _token_stride(q, "q")
+    B, T, Hq, D = q.shape
+    ks, Hkv = 0, 0
+    if k is not None:
+        ks, Hkv = _token_stride(k, "k"), k.shape[2]
+        if tuple(k.shape) != (B, T, Hkv, D):
+            raise ValueError(f"k: expected [{B},{T},Hkv,{D}], got {tuple(k.shape)}")
+    if positions is None:
+        raise ValueError("positions must be [axes,B,T]")
+    rot = _rotation(freqs, positions, offsets, axes, pairs, B, T)
+    if out is None:
+        out = (torch.empty((B, T, Hq, D), dtype=q.dtype, device=q.device),
+               None if k is None else torch.empty((B, T, Hkv, D), dtype=q.dtype, device=q.device))
+    qo, ko = out
+    _want(qo, torch.bfloat16, (B, T, Hq, D), "q_out", True)
+    if (k is None) != (ko is None):
+        raise ValueError("out: k and its place go together")
+    if ko is not None:
+        _want(ko, torch.bfloat16, (B, T, Hkv, D), "k_out", True)
+    _same_device(q, k, freqs, positions, offsets, qo, ko)
+    p = RotaryParams(B, T, Hq, Hkv, D, qs, ks)
+    with torch.cuda.device(q.device):
+        _check(lib().gsd_rotary(q.data_ptr(), _ptr(k), freqs.data_ptr(), positions.data_ptr(), _ptr(offsets), qo.data_ptr(),
+                                _ptr(ko), ctypes.byref(p), ctypes.byref(rot), _stream(q)))
+    return qo, ko
 
 
 def gsd_token_logprobs_workspace_bytes(B, N, V, T, k=0) -> int:

@@ -366,6 +366,67 @@ extern "C" int gsd_verify_attn_q8(const void* q, const void* k_cache, const void
     return rc;
 }
 
+// ---------------------------------------------------------------- the same over a paged cache
+namespace {
+int attn_paged_params_ok(const gsd_attn_params* p, const gsd_page_params* c) {
+    const int ok = attn_params_ok(p);
+    if (ok != GSD_OK) return ok;
+    if (!c) return GSD_ERR_NULL_POINTER;
+    if (p->kernel == GSD_ATTN_TCGEN05 && 128 % (p->Hq / p->Hkv) != 0) {
+        set_error_text("GSD_ATTN_TCGEN05 needs D == 128 and a group size that divides 128");
+        return GSD_ERR_UNSUPPORTED;
+    }
+    return page_rows_log2(c, p->Lmax) < 0 ? GSD_ERR_BAD_SHAPE : GSD_OK;
+}
+AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
+    gsd_attn_params as = *p;
+    as.num_splits = std::max(p->num_splits, 0);
+    return attn_make_plan(&as, sm_count);
+}
+}  // namespace
+
+extern "C" size_t gsd_verify_attn_paged_workspace_bytes(const gsd_attn_params* p, const gsd_page_params* c) {
+    if (attn_paged_params_ok(p, c) != GSD_OK) return 0;
+    DeviceInfo di;
+    if (device_info(&di) != 0) return 0;
+    return attn_paged_make_plan(p, di.sm_count).ws_bytes;
+}
+
+extern "C" int gsd_verify_attn_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                                     const void* draft_k, const void* draft_v, const uint32_t* ancestor_mask,
+                                     const int32_t* seq_lens, void* out, const gsd_attn_params* p, const gsd_page_params* c,
+                                     void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+    if (!p || !c || !q || !k_pages || !v_pages || !page_table || !draft_k || !draft_v || !ancestor_mask || !seq_lens || !out)
+        return GSD_ERR_NULL_POINTER;
+    const int ok = attn_paged_params_ok(p, c);
+    if (ok != GSD_OK) return ok;
+    for (const void* ptr : {q, k_pages, v_pages, draft_k, draft_v, (const void*)out})
+        if (((uintptr_t)ptr & 15u) != 0) return GSD_ERR_MISALIGNED;
+    for (const void* ptr : {(const void*)page_table, (const void*)ancestor_mask, (const void*)seq_lens})
+        if (((uintptr_t)ptr & 3u) != 0) return GSD_ERR_MISALIGNED;
+    DeviceInfo di;
+    if (device_info(&di) != 0) return GSD_ERR_CUDA;
+    const AttnPlan plan = attn_paged_make_plan(p, di.sm_count);
+    if (plan.ws_bytes > 0) {
+        if (!workspace || workspace_bytes < plan.ws_bytes) return GSD_ERR_WORKSPACE;
+        if (((uintptr_t)workspace & 255u) != 0) return GSD_ERR_MISALIGNED;
+    }
+    AttnArgs a;
+    a.q = q; a.k_cache = k_pages; a.v_cache = v_pages; a.draft_k = draft_k; a.draft_v = draft_v;
+    a.mask = ancestor_mask; a.seq_lens = seq_lens; a.out = out;
+    a.B = p->B; a.N = p->N; a.Hq = p->Hq; a.Hkv = p->Hkv; a.D = p->D; a.Lmax = p->Lmax;
+    a.G = p->Hq / p->Hkv; a.W = (p->N + 31) / 32;
+    const float scale = p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->D);
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.plan = plan; a.workspace = workspace; a.status = status;
+    a.stream = (cudaStream_t)stream;
+    a.pages.table = page_table; a.pages.page_log2 = page_rows_log2(c, p->Lmax);
+    a.pages.max_pages = c->max_pages; a.pages.num_pages = c->num_pages;
+    int rc = plan.kernel == GSD_ATTN_TCGEN05 ? launch_attn_tcgen05(a) : launch_attn_mma(a);
+    if (rc == GSD_OK && plan.slots > 0) rc = launch_attn_merge(a);
+    return rc;
+}
+
 // ---------------------------------------------------------------- host-buffer step
 namespace {
 struct ArenaLayout {

@@ -139,6 +139,17 @@ struct Kv8Args {            // a cache held in 8 bits (gsd_verify_attn_q8)
     int blocks, block_log2; // scale blocks of a sequence, log2 of the tokens of one
     bool int8;              // codes: int8, else e4m3
 };
+// log2 of the rows of a page, or -1 if the sizes are not those of a paged cache that has room for Lmax rows a sequence.
+inline int page_rows_log2(const gsd_page_params* c, int Lmax) {
+    if (c->num_pages < 1 || c->max_pages < 1 || Lmax > (1 << 30)) return -1;
+    for (int k = 4; k <= 8; ++k)
+        if (c->page == 1 << k) return (long long)c->max_pages << k >= Lmax ? k : -1;
+    return -1;
+}
+struct PageArgs {           // a cache held in pages (gsd_verify_attn_paged); k_cache and v_cache are the pool
+    const int32_t* table;   // nullptr: the cache is not paged
+    int page_log2, max_pages, num_pages;
+};
 struct AttnArgs {
     const void *q, *k_cache, *v_cache, *draft_k, *draft_v;
     const uint32_t* mask;
@@ -151,6 +162,7 @@ struct AttnArgs {
     int32_t* status;
     cudaStream_t stream;
     Kv8Args kv8;
+    PageArgs pages = {};
 };
 
 int attn_pick_kernel(const gsd_attn_params* p, int sm_count);   // GSD_ATTN_MMA or GSD_ATTN_TCGEN05
@@ -213,6 +225,7 @@ int launch_kv8_expand(const AttnArgs& a, void* k_out, void* v_out, void* draft_v
 int attn_q8_mma_rows(int R);                  // stacked rows of one of its items
 int attn_q8_mma_resident(int R, int D);              // its CTAs an SM holds
 int launch_attn_tcgen05(const AttnArgs& a);
+int launch_attn_tcgen05_paged(const AttnArgs& a, bool long_mask);   // (called by launch_attn_tcgen05)
 bool attn_tcgen05_supports(int D, int G);
 int attn_tcgen05_rows(int G);                 // stacked rows of one row tile
 int launch_attn_merge(const AttnArgs& a);

@@ -39,16 +39,26 @@ struct Table {
     decltype(&gsd_append_kv_q8) append_kv_q8;
     decltype(&gsd_token_logprobs) token_logprobs;
     decltype(&gsd_token_logprobs_workspace_bytes) token_logprobs_workspace_bytes;
+    decltype(&gsd_verify_attn_paged) verify_attn_paged;
+    decltype(&gsd_verify_attn_paged_workspace_bytes) verify_attn_paged_workspace_bytes;
+    decltype(&gsd_commit_kv_paged) commit_kv_paged;
+    decltype(&gsd_append_kv_paged) append_kv_paged;
+    decltype(&gsd_rotary) rotary;
 };
 constexpr Py_ssize_t kTable = sizeof(Table) / sizeof(void*);
 Table g;       // written under the GIL by bind(), copied under the GIL by every call
 
-// A tensor that the C ABI can take as it is; nullptr otherwise.
-const at::Tensor* plain(PyObject* o) {
+// A CUDA tensor with its own memory; nullptr otherwise.
+const at::Tensor* strided(PyObject* o) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || at::isTensorSubclassLike(t) || !t.is_contiguous()) return nullptr;
+    if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || at::isTensorSubclassLike(t)) return nullptr;
     return &t;
+}
+// A tensor that the C ABI can take as it is; nullptr otherwise.
+const at::Tensor* plain(PyObject* o) {
+    const at::Tensor* t = strided(o);
+    return t && t->is_contiguous() ? t : nullptr;
 }
 
 // Collects the arguments of one call; `ok` turns false at the first that is not the plain case.
@@ -531,11 +541,202 @@ PyObject* py_token_logprobs(PyObject*, PyObject* const* argv, Py_ssize_t nargs) 
     GSD_PY_END
 }
 
+// The paged cache that argument `at` begins (k_pages, v_pages, page_table).
+struct Pages {
+    gsd_page_params c;
+    const at::Tensor *k, *v, *table;
+    int32_t B, Hkv, D, Lmax;
+};
+bool pages_args(Args& a, int at, Pages& s) {
+    s.k = a.tensor(at, at::kBFloat16, 4);
+    s.table = a.tensor(at + 2, at::kInt, 2);
+    if (!a.ok) return false;
+    s.c.num_pages = a.size(s.k, 0); s.c.page = a.size(s.k, 1); s.Hkv = a.size(s.k, 2); s.D = a.size(s.k, 3);
+    s.B = a.size(s.table, 0); s.c.max_pages = a.size(s.table, 1);
+    if (!a.ok || s.c.page < 16 || s.c.page > 256 || (s.c.page & (s.c.page - 1)) != 0) return a.ok = false;
+    s.v = a.tensor(at + 1, at::kBFloat16, {s.c.num_pages, s.c.page, s.Hkv, s.D});
+    s.Lmax = (int32_t)std::min<int64_t>((int64_t)s.c.max_pages * s.c.page, 1 << 30);
+    return a.ok;
+}
+
+// (q, k_pages, v_pages, page_table, draft_k, draft_v, mask, seq_lens, out, max_len, scale, num_splits, kernel, workspace, status)
+PyObject* py_verify_attn_paged(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(15)
+    const at::Tensor* q = a.tensor(0, at::kBFloat16, 4);
+    Pages s;
+    if (!a.ok || !pages_args(a, 1, s)) Py_RETURN_NONE;
+    gsd_attn_params p;
+    p.B = a.size(q, 0); p.N = a.size(q, 1); p.Hq = a.size(q, 2); p.D = a.size(q, 3);
+    p.Hkv = s.Hkv;
+    const int32_t max_len = a.i32(9);
+    p.Lmax = max_len ? max_len : s.Lmax;
+    GSD_PY_PLAIN;
+    if (s.B != p.B || s.D != p.D) Py_RETURN_NONE;
+    const at::Tensor* dk = a.tensor(4, at::kBFloat16, {p.B, p.N, p.Hkv, p.D});
+    const at::Tensor* dv = a.tensor(5, at::kBFloat16, {p.B, p.N, p.Hkv, p.D});
+    const at::Tensor* sl = a.tensor(7, at::kInt, {p.B});
+    GSD_PY_PLAIN;
+    const at::Tensor* mask = plain(argv[6]);
+    if (!mask || mask->get_device() != a.device || (mask->scalar_type() != at::kInt && mask->scalar_type() != at::kUInt32) ||
+        !mask->sizes().equals({p.B, p.N, ((int64_t)p.N + 31) / 32}))
+        Py_RETURN_NONE;
+    const at::Tensor* out = argv[8] == Py_None ? nullptr : a.tensor(8, at::kBFloat16, {p.B, p.N, p.Hq, p.D});
+    p.softmax_scale = a.f32(10); p.num_splits = a.i32(11); p.kernel = a.i32(12);
+    const at::Tensor* ws = a.any_or_none(13);
+    const at::Tensor* status = a.any_or_none(14);
+    GSD_PY_PLAIN;
+    Call c(a.device);
+    at::Tensor made;
+    if (!out) {
+        made = empty(q->sizes(), at::kBFloat16, a.device);
+        out = &made;
+    }
+    c.scratch(ws, ws ? 0 : lib.verify_attn_paged_workspace_bytes(&p, &s.c), a.device);
+    const int rc = unlocked([&] {
+        return lib.verify_attn_paged(ptr<void>(q), ptr<void>(s.k), ptr<void>(s.v), ptr<int32_t>(s.table), ptr<void>(dk), ptr<void>(dv),
+                                     ptr<uint32_t>(mask), ptr<int32_t>(sl), ptr<void>(out), &p, &s.c, c.ws, c.ws_bytes,
+                                     ptr<int32_t>(status), c.stream);
+    });
+    if (rc != GSD_OK) return PyLong_FromLong(rc);
+    if (!made.defined()) {
+        Py_INCREF(argv[8]);
+        return argv[8];
+    }
+    return THPVariable_Wrap(std::move(made));
+    GSD_PY_END
+}
+
+// (k_pages, v_pages, page_table, draft_k, draft_v, accepted_nodes, accepted_len, seq_lens, status); returns 0 when done
+PyObject* py_commit_kv_paged(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(9)
+    Pages s;
+    if (!pages_args(a, 0, s)) Py_RETURN_NONE;
+    const at::Tensor* dk = a.tensor(3, at::kBFloat16, 4);
+    const at::Tensor* nodes = a.tensor(5, at::kInt, 2);
+    GSD_PY_PLAIN;
+    gsd_commit_params p;
+    p.B = s.B; p.Lmax = s.Lmax; p.Hkv = s.Hkv; p.D = s.D;
+    p.N = a.size(dk, 1); p.Tcap = a.size(nodes, 1);
+    GSD_PY_PLAIN;
+    if (nodes->size(0) != p.B || !dk->sizes().equals({p.B, p.N, p.Hkv, p.D})) Py_RETURN_NONE;
+    const at::Tensor* dv = a.tensor(4, at::kBFloat16, {p.B, p.N, p.Hkv, p.D});
+    const at::Tensor* len = a.tensor(6, at::kInt, {p.B});
+    const at::Tensor* sl = a.tensor(7, at::kInt, {p.B});
+    const at::Tensor* status = a.any_or_none(8);
+    GSD_PY_PLAIN;
+    Call c(a.device);
+    return PyLong_FromLong(unlocked([&] {
+        return lib.commit_kv_paged(ptr<void>(s.k), ptr<void>(s.v), ptr<int32_t>(s.table), ptr<void>(dk), ptr<void>(dv), ptr<int32_t>(nodes),
+                                   ptr<int32_t>(len), ptr<int32_t>(sl), &p, &s.c, ptr<int32_t>(status), c.stream);
+    }));
+    GSD_PY_END
+}
+
+// Argument i as rows [B, T, H, D] bf16 whose rows of a token are contiguous; `stride`: elements from a token to the next.
+const at::Tensor* rows_arg(Args& a, int i, int64_t* stride) {
+    const at::Tensor* t = a.ok ? strided(a.v[i]) : nullptr;
+    if (!t || t->scalar_type() != at::kBFloat16 || t->dim() != 4 || (a.device >= 0 && t->get_device() != a.device)) {
+        a.ok = false;
+        return nullptr;
+    }
+    a.device = (int)t->get_device();
+    const int64_t B = t->size(0), T = t->size(1), H = t->size(2), D = t->size(3);
+    const int64_t s = T > 1 ? t->stride(1) : B > 1 ? t->stride(0) : H * D;
+    if (t->stride(3) != 1 || (H > 1 && t->stride(2) != D) || (B > 1 && t->stride(0) != T * s)) a.ok = false;
+    *stride = s;
+    return t;
+}
+// The rotation of arguments freqs, positions, offsets, axes, pairs from `at` on, for B x T tokens.
+struct Turn {
+    gsd_rotation r;
+    const at::Tensor *freqs, *positions, *offsets;
+};
+bool turn_args(Args& a, int at, int32_t B, int32_t T, Turn& s) {
+    s.freqs = a.tensor(at, at::kFloat, 1);
+    s.positions = a.v[at + 1] == Py_None ? nullptr : a.tensor(at + 1, at::kInt, 3);
+    s.offsets = a.v[at + 2] == Py_None ? nullptr : a.tensor(at + 2, at::kInt, {B});
+    if (!a.ok || s.freqs->size(0) > 64 || (s.positions && (s.positions->size(1) != B || s.positions->size(2) != T))) return a.ok = false;
+    s.r.pairs = (int32_t)s.freqs->size(0);
+    s.r.axes = s.positions ? a.size(s.positions, 0) : 1;
+    if (a.v[at + 4] != Py_True && a.v[at + 4] != Py_False) return a.ok = false;
+    s.r.layout = a.v[at + 4] == Py_True ? GSD_ROTARY_NEIGHBOURS : GSD_ROTARY_HALVES;
+    memset(s.r.axis, 0, sizeof s.r.axis);
+    PyObject* axes = a.v[at + 3];
+    if (axes == Py_None) return true;
+    if ((!PyList_CheckExact(axes) && !PyTuple_CheckExact(axes)) || PySequence_Fast_GET_SIZE(axes) != s.r.pairs) return a.ok = false;
+    for (int32_t i = 0; i < s.r.pairs; ++i) {
+        PyObject* o = PySequence_Fast_GET_ITEM(axes, i);
+        int overflow = 0;
+        const long x = PyLong_CheckExact(o) ? PyLong_AsLongAndOverflow(o, &overflow) : -1;
+        if (overflow || x < 0 || x >= (s.positions ? s.r.axes : GSD_ROTARY_MAX_AXES)) return a.ok = false;
+        s.r.axis[i] = (uint8_t)x;
+        if (x >= s.r.axes) s.r.axes = (int32_t)x + 1;
+    }
+    return true;
+}
+
+// (k_pages, v_pages, page_table, k, v, counts, seq_lens, freqs, positions, offsets, axes, pairs, status); returns 0 when done
+PyObject* py_append_kv_paged(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(13)
+    Pages s;
+    if (!pages_args(a, 0, s)) Py_RETURN_NONE;
+    gsd_append_paged_params p;
+    const at::Tensor* k = rows_arg(a, 3, &p.k_stride);
+    const at::Tensor* v = rows_arg(a, 4, &p.v_stride);
+    GSD_PY_PLAIN;
+    p.B = s.B; p.Lmax = s.Lmax; p.Hkv = s.Hkv; p.D = s.D;
+    p.T = a.size(k, 1);
+    GSD_PY_PLAIN;
+    if (!k->sizes().equals({p.B, p.T, p.Hkv, p.D}) || !v->sizes().equals(k->sizes())) Py_RETURN_NONE;
+    const at::Tensor* counts = a.tensor(5, at::kInt, {p.B});
+    const at::Tensor* sl = a.tensor(6, at::kInt, {p.B});
+    Turn turn{};
+    const bool turned = argv[7] != Py_None;
+    if (turned ? !turn_args(a, 7, p.B, p.T, turn) : argv[8] != Py_None || argv[9] != Py_None || argv[10] != Py_None) Py_RETURN_NONE;
+    const at::Tensor* status = a.any_or_none(12);
+    GSD_PY_PLAIN;
+    Call c(a.device);
+    return PyLong_FromLong(unlocked([&] {
+        return lib.append_kv_paged(ptr<void>(s.k), ptr<void>(s.v), ptr<int32_t>(s.table), ptr<void>(k), ptr<void>(v), ptr<int32_t>(counts),
+                                   ptr<int32_t>(sl), ptr<float>(turn.freqs), ptr<int32_t>(turn.positions), ptr<int32_t>(turn.offsets), &p,
+                                   &s.c, turned ? &turn.r : nullptr, ptr<int32_t>(status), c.stream);
+    }));
+    GSD_PY_END
+}
+
+// (q, k, freqs, positions, offsets, axes, pairs, out)
+PyObject* py_rotary(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
+    GSD_PY_BEGIN(8)
+    if (argv[7] != Py_None || argv[3] == Py_None) Py_RETURN_NONE;
+    gsd_rotary_params p = {};
+    const at::Tensor* q = rows_arg(a, 0, &p.q_stride);
+    const at::Tensor* k = argv[1] == Py_None ? nullptr : rows_arg(a, 1, &p.k_stride);
+    GSD_PY_PLAIN;
+    p.B = a.size(q, 0); p.T = a.size(q, 1); p.Hq = a.size(q, 2); p.D = a.size(q, 3);
+    if (k) p.Hkv = a.size(k, 2);
+    GSD_PY_PLAIN;
+    if (k && !k->sizes().equals({p.B, p.T, p.Hkv, p.D})) Py_RETURN_NONE;
+    Turn turn{};
+    if (!turn_args(a, 2, p.B, p.T, turn)) Py_RETURN_NONE;
+    Call c(a.device);
+    at::Tensor qo = empty(q->sizes(), at::kBFloat16, a.device), ko;
+    if (k) ko = empty(k->sizes(), at::kBFloat16, a.device);
+    const int rc = unlocked([&] {
+        return lib.rotary(ptr<void>(q), ptr<void>(k), ptr<float>(turn.freqs), ptr<int32_t>(turn.positions), ptr<int32_t>(turn.offsets),
+                          ptr<void>(&qo), k ? ptr<void>(&ko) : nullptr, &p, &turn.r, c.stream);
+    });
+    if (rc != GSD_OK) return PyLong_FromLong(rc);
+    PyObject* second = k ? THPVariable_Wrap(ko) : Py_NewRef(Py_None);
+    return tuple_of({THPVariable_Wrap(qo), second});
+    GSD_PY_END
+}
+
 #define GSD_PY_FN(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {GSD_PY_FN(bind), GSD_PY_FN(verify_attn), GSD_PY_FN(accept), GSD_PY_FN(accept_sampled),
                          GSD_PY_FN(draft_expand), GSD_PY_FN(build_mask), GSD_PY_FN(commit_kv),
                          GSD_PY_FN(verify_attn_q8), GSD_PY_FN(commit_kv_q8), GSD_PY_FN(append_kv_q8),
-                         GSD_PY_FN(token_logprobs), {nullptr, nullptr, 0, nullptr}};
+                         GSD_PY_FN(token_logprobs), GSD_PY_FN(verify_attn_paged), GSD_PY_FN(commit_kv_paged),
+                         GSD_PY_FN(append_kv_paged), GSD_PY_FN(rotary), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
