@@ -378,10 +378,46 @@ int attn_paged_params_ok(const gsd_attn_params* p, const gsd_page_params* c) {
     }
     return page_rows_log2(c, p->Lmax) < 0 ? GSD_ERR_BAD_SHAPE : GSD_OK;
 }
+// The kernel for few rows reads the cache once for 32 rows (64 at D = 64); the tcgen05 kernel for up to 256.
+int attn_paged_pick_kernel(const gsd_attn_params* p) {
+    if (p->kernel != GSD_ATTN_AUTO) return p->kernel;
+    const int G = p->Hq / p->Hkv, R = p->N * G;
+    return attn_tcgen05_supports(p->D, G) && R > (p->D == 64 ? 64 : 32) ? GSD_ATTN_TCGEN05 : GSD_ATTN_MMA;
+}
 AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
-    gsd_attn_params as = *p;
-    as.num_splits = std::max(p->num_splits, 0);
-    return attn_make_plan(&as, sm_count);
+    if (attn_paged_pick_kernel(p) == GSD_ATTN_TCGEN05) {
+        gsd_attn_params as = *p;
+        as.kernel = GSD_ATTN_TCGEN05;
+        as.num_splits = std::max(p->num_splits, 0);
+        return attn_make_plan(&as, sm_count);
+    }
+    AttnPlan pl = {};
+    const int R = p->N * (p->Hq / p->Hkv);
+    pl.kernel = GSD_ATTN_MMA;
+    pl.rows_per_item = attn_paged_rows(R, p->D);
+    pl.part_rows = 64;
+    pl.dev.tiles_per_unit = (R + pl.rows_per_item - 1) / pl.rows_per_item;
+    pl.items = pl.dev.tiles_per_unit * p->B * p->Hkv;
+    pl.dev.items_a = pl.items;
+    pl.dev.splits_a = pl.dev.splits_b = 1;
+    const int resident = sm_count * attn_paged_rows_resident(R, p->D);
+    const int rounds = ((p->Lmax + 15) / 16 + (p->N + 15) / 16 + 7) / 8;        // of a tile for each warp
+    if (p->num_splits > 0) {
+        pl.dev.splits_a = p->num_splits;
+    } else if (pl.items + p->Hkv * pl.dev.tiles_per_unit <= resident && rounds > 2 && p->B <= 32) {
+        // the kernel deals the work out by length; all items of a sequence are cut alike, so with fewer CTAs to spare than a
+        // sequence has items there is nothing to cut
+        pl.dev.balanced = 3;
+        pl.ctas = pl.slots = resident;                  // unit w owns slot w
+        pl.ws_bytes = plan_part_o_bytes(pl, p->D) + plan_part_ml_bytes(pl) + plan_bal_bytes(pl, p->B);
+        return pl;
+    } else if (pl.items < resident) {
+        pl.dev.splits_a = std::max(1, std::min({resident / pl.items, rounds / 2, 64}));
+    }
+    pl.ctas = pl.items * pl.dev.splits_a;
+    pl.slots = pl.dev.splits_a > 1 ? pl.ctas : 0;
+    pl.ws_bytes = pl.slots ? plan_part_o_bytes(pl, p->D) + plan_part_ml_bytes(pl) : 0;
+    return pl;
 }
 }  // namespace
 
@@ -422,7 +458,7 @@ extern "C" int gsd_verify_attn_paged(const void* q, const void* k_pages, const v
     a.stream = (cudaStream_t)stream;
     a.pages.table = page_table; a.pages.page_log2 = page_rows_log2(c, p->Lmax);
     a.pages.max_pages = c->max_pages; a.pages.num_pages = c->num_pages;
-    int rc = plan.kernel == GSD_ATTN_TCGEN05 ? launch_attn_tcgen05(a) : launch_attn_mma(a);
+    int rc = plan.kernel == GSD_ATTN_TCGEN05 ? launch_attn_tcgen05(a) : launch_attn_paged_rows(a);
     if (rc == GSD_OK && plan.slots > 0) rc = launch_attn_merge(a);
     return rc;
 }

@@ -256,7 +256,8 @@ int launch_attn_merge(const AttnArgs& a) {
     if (device_info(&di) != 0) return GSD_ERR_CUDA;
     const bool few = blocks <= (long)kBlocksFew * di.sm_count;
     void (*kernel)(MergeParams) = nullptr;
-    if (rows == 8) kernel = few ? attn_merge_kernel<false, 8, true> : attn_merge_kernel<false, 8, false>;    // (the mma.sync kernel has no one-wave plan)
+    if (rows == 8 && walk) kernel = few ? attn_merge_kernel<true, 8, true> : attn_merge_kernel<true, 8, false>;
+    else if (rows == 8) kernel = few ? attn_merge_kernel<false, 8, true> : attn_merge_kernel<false, 8, false>;
     else if (walk) kernel = few ? attn_merge_kernel<true, 32, true> : attn_merge_kernel<true, 32, false>;
     else kernel = few ? attn_merge_kernel<false, 32, true> : attn_merge_kernel<false, 32, false>;
     int threads = kThreads;

@@ -76,12 +76,9 @@ struct MmaParams {
     int B, N, Hq, Hkv, Lmax, G, W, R;
     int slots;       // partial-result slots of the plan
     float scale_log2;
-    PageArgs pages;  // PAGED kernels only
 };
 
-// PAGED: the cache lies in pages (k_cache, v_cache: the pool).  A tile's rows are in four runs of 16, each within one page; lane i
-// of every warp looks up the page of run i & 3 of the next tile while the present one is worked on.
-template <int D, int KEY_WARPS, bool PAGED>
+template <int D, int KEY_WARPS>
 __global__ void __launch_bounds__(kThreads) attn_mma_kernel(MmaParams p) {
     constexpr int CH = D / 8;              // 16-byte chunks per row
     constexpr int TILE = BN * D * 2;       // bytes of one K or V tile
@@ -166,32 +163,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(MmaParams p) {
     auto tile_live = [&](int t) -> bool {
         return t < nPT || ((live_tiles >> (t - nPT)) & 1u);
     };
-    // PAGED: the first row of the pool that the lane's run of tile t lies in; -1 where nothing is to be read
-    auto find_run = [&](int t) -> long long {
-        const int key = t * BN + (lane & 3) * 16;
-        if (t >= nPT || key >= L || !GSD_IN_BOUNDS(key >> p.pages.page_log2 < p.pages.max_pages, p.status)) return -1;
-        const int page = p.pages.table[(size_t)b * p.pages.max_pages + (key >> p.pages.page_log2)];
-        if ((unsigned)page >= (unsigned)p.pages.num_pages) {
-            if (p.status) atomicOr((unsigned*)p.status, GSD_DEV_BAD_PAGE);
-            return -1;
-        }
-        return ((long long)page << p.pages.page_log2) + (key & ((1 << p.pages.page_log2) - 1));
-    };
-    auto load_paged_tile = [&](int t, int stage, long long run) {
-        const size_t rstride = (size_t)p.Hkv * D;
-#pragma unroll
-        for (int x = 0; x < BN * CH / kThreads; ++x) {
-            const int i = x * kThreads + tid, r = i / CH, ch = i % CH;
-            const long long at = __shfl_sync(0xFFFFFFFFu, run, r >> 4);
-            const bool ok = at >= 0 && t * BN + r < L;
-            const size_t off = ok ? ((size_t)at + (r & 15)) * rstride + (size_t)c * D + ch * 8 : 0;
-            cp_async16(smem_u32(sK(stage) + tile_off<D>(r, ch)), p.k_cache + off, ok ? 16 : 0);
-            cp_async16(smem_u32(sV(stage) + tile_off<D>(r, ch)), p.v_cache + off, ok ? 16 : 0);
-        }
-    };
-    long long run = 0;                       // of the next tile to be loaded
     auto load_tile = [&](int t, int stage) {
-        if (PAGED && t < nPT) return load_paged_tile(t, stage, run);
         const bool draft = t >= nPT;
         const int key0 = (draft ? t - nPT : t) * BN;
         const int limit = draft ? N : L;
@@ -229,15 +201,12 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(MmaParams p) {
     // than that: 8 x 32 heads, N 40, L 1500 56.7 -> 57.4).  Warps that share the keys of a tile all have rows.
     const bool active = KEY_WARPS > 1 || row0 + warp * 16 < R;
     int t = next_live(t_begin);
-    if (PAGED) run = find_run(t);
     if (t < t_end) load_tile(t, 0);
-    if (PAGED) run = find_run(t + 1);
     cp_async_commit();
     int stage = 0;
     while (t < t_end) {
         const int t_next = next_live(t + 1);
         if (t_next < t_end) load_tile(t_next, stage ^ 1);
-        if (PAGED) run = find_run(t_next + 1);
         cp_async_commit();
         cp_async_wait<1>();
         __syncthreads();
@@ -440,7 +409,7 @@ __global__ void __launch_bounds__(kThreads) attn_mma_kernel(MmaParams p) {
     }
 }
 
-template <int D, int KEY_WARPS, bool PAGED>
+template <int D, int KEY_WARPS>
 int launch_mma_t(const AttnArgs& a) {
     MmaParams p;
     p.q = (const __nv_bfloat16*)a.q; p.k_cache = (const __nv_bfloat16*)a.k_cache;
@@ -449,7 +418,6 @@ int launch_mma_t(const AttnArgs& a) {
     p.out = (__nv_bfloat16*)a.out; p.status = a.status;
     p.B = a.B; p.N = a.N; p.Hq = a.Hq; p.Hkv = a.Hkv; p.Lmax = a.Lmax; p.G = a.G; p.W = a.W;
     p.R = a.N * a.G; p.scale_log2 = a.scale_log2; p.plan = a.plan.dev; p.slots = a.plan.slots;
-    p.pages = a.pages;
     p.part_o = (float*)a.workspace;
     p.part_ml = (float*)((char*)a.workspace + plan_part_o_bytes(a.plan, a.D));
     const int smem = 4 * BN * D * 2;
@@ -458,29 +426,24 @@ int launch_mma_t(const AttnArgs& a) {
         int dev = 0;
         GSD_CUDA_TRY(cudaGetDevice(&dev));
         if (dev < 0 || dev >= 64 || !done[dev]) {
-            GSD_CUDA_TRY(cudaFuncSetAttribute(attn_mma_kernel<D, KEY_WARPS, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+            GSD_CUDA_TRY(cudaFuncSetAttribute(attn_mma_kernel<D, KEY_WARPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
             if (dev >= 0 && dev < 64) done[dev] = true;
         }
     }
-    GSD_CUDA_TRY(launch_dependent(attn_mma_kernel<D, KEY_WARPS, PAGED>, dim3(a.plan.ctas), dim3(kThreads), smem, a.stream, p));
+    GSD_CUDA_TRY(launch_dependent(attn_mma_kernel<D, KEY_WARPS>, dim3(a.plan.ctas), dim3(kThreads), smem, a.stream, p));
     return GSD_OK;
 }
 
 }  // namespace
 
-template <bool PAGED>
-static int launch_mma(const AttnArgs& a) {
+int launch_attn_mma(const AttnArgs& a) {
     // Few rows leave warps without any: two or four of them then share the 64 keys of a tile.  Among other passes, one
     // warp for all keys -> shared: 8 x 32 heads, N 8, L 64 / 200 / 1000 7.2 / 12.0 / 32.5 -> 6.4 / 9.5 / 25.4 us; N 32, L 64
     // / 1000 / 4000 9.0 / 41.2 / 137.7 -> 8.1 / 30.8 / 95.5; D 64, 32 x 32/8, N 8, L 1500 47.3 -> 31.0.
     const int rows = a.N * a.G;
-    if (a.D == 128)
-        return rows <= 16 ? launch_mma_t<128, 4, PAGED>(a) : rows <= 32 ? launch_mma_t<128, 2, PAGED>(a) : launch_mma_t<128, 1, PAGED>(a);
-    if (a.D == 64)
-        return rows <= 16 ? launch_mma_t<64, 4, PAGED>(a) : rows <= 32 ? launch_mma_t<64, 2, PAGED>(a) : launch_mma_t<64, 1, PAGED>(a);
+    if (a.D == 128) return rows <= 16 ? launch_mma_t<128, 4>(a) : rows <= 32 ? launch_mma_t<128, 2>(a) : launch_mma_t<128, 1>(a);
+    if (a.D == 64) return rows <= 16 ? launch_mma_t<64, 4>(a) : rows <= 32 ? launch_mma_t<64, 2>(a) : launch_mma_t<64, 1>(a);
     return GSD_ERR_BAD_SHAPE;
 }
-
-int launch_attn_mma(const AttnArgs& a) { return a.pages.table ? launch_mma<true>(a) : launch_mma<false>(a); }
 
 }  // namespace gsd

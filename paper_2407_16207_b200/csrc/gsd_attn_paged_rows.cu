@@ -1,0 +1,495 @@
+// gsd_verify_attn_paged, warp-level back end for few stacked rows (single tokens, small draft graphs): attention over a bf16
+// cache held in pages.
+//
+//   s_j = scale <q, K_j>,   p_j = 2^(s_j log2(e) - m),   out = sum_j p_j V_j / sum_j p_j
+//
+// A tile is 16 keys: a page holds whole tiles, so each lies in one place.  Every warp has tiles of its own, a ring of them in
+// shared memory filled by asynchronous copies, and nothing to wait for but its own; the warps meet once, at the end.  Lane l of
+// a warp looks up the page of the l-th of its next 32 tiles.  Both products are transposed, S^T = K Q^T and O^T = V^T P^T, so
+// that 8 rows fill an instruction (16 keys or 16 columns by 8 rows); the weights are turned round by a movmatrix.  A row's
+// running maximum is raised when a score exceeds it by more than 2^kLag: the weights are rounded to bf16, whose relative
+// step does not depend on their size, and sums stay fp32.
+//
+// The work is dealt out by length inside the kernel for up to 32 sequences: every item (a group of rows of a sequence and
+// kv head) is cut into ranges of at most T rounds of keys, T the least with which all ranges are resident at once.
+#include "gsd_internal.cuh"
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+namespace gsd {
+namespace {
+
+constexpr int kKeys = 16;                    // keys of a warp's tile
+constexpr float kLag = 8.f;                  // log2
+
+struct RowsParams {
+    const __nv_bfloat16 *q, *k_pages, *v_pages, *draft_k, *draft_v;
+    const uint32_t* mask;
+    const int32_t* seq_lens;
+    __nv_bfloat16* out;
+    float* part_o;   // [slot][D / 4][64] float4
+    float* part_ml;  // [slot][64][2]
+    int* left;       // plan by length: split counts and first units for the merge pass
+    int left_off;
+    PlanDev plan;
+    PageArgs pages;
+    int32_t* status;
+    int B, N, Hq, Hkv, Lmax, G, W, R;
+    int slots;
+    float scale_log2;
+};
+
+template <int D, int NT>
+struct RowsGeo {
+    static constexpr int WARPS = 8;
+    static constexpr int THREADS = 32 * WARPS;
+    static constexpr int ROWS = 8 * NT;                         // stacked rows of an item
+    static constexpr int TILE = kKeys * D * 2;                  // bytes of a K or V tile
+    static constexpr int BLOCKS = D == 64 && NT <= 2 ? 2 : 1;   // CTAs an SM
+    static constexpr int STAGES = D == 128 ? 3 : BLOCKS == 2 ? 3 : 5;
+    static constexpr int RING = WARPS * STAGES * 2 * TILE;
+    static constexpr int MTILES = D / 16;                       // output tiles of 16 columns
+    static constexpr int VALUES = MTILES * 4 + 4;               // of a lane and 8 rows, when the warps' results are brought together
+    static constexpr int MEET = WARPS * NT * VALUES * 32 * 4;
+    static constexpr int Q_AT = RING > MEET ? RING : MEET;      // query fragments: [row group][k-step][lane] pairs of registers
+    static constexpr int SMEM = Q_AT + NT * (D / 16) * 32 * 8;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16-byte async copy; src_bytes == 0 writes zeros and reads nothing
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+// 8x8 bf16 values, a row a quarter of lanes -> their transpose.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+
+// What a CTA works on: rows of (sequence b, kv head c), keys of one of `nsplit` ranges.
+struct Unit {
+    int b, c, row0, split, nsplit, slot, L;
+};
+
+__device__ __forceinline__ int visible_len(const RowsParams& p, int b) {
+    const int L = p.seq_lens[b];
+    return L < 0 ? 0 : (L > p.Lmax ? p.Lmax : L);
+}
+
+// Plan by length, made by every warp for itself, a lane per sequence: the cut of each sequence's items into ranges of at most T
+// rounds (a tile for each warp); unit w is this CTA's, if there are that many.  `leave`: the merge pass's tables are written.
+template <int kRound>
+__device__ __forceinline__ bool unit_by_length(const RowsParams& p, int w, int lane, bool leave, Unit& u) {
+    const unsigned all = 0xFFFFFFFFu;
+    const bool in = lane < p.B;
+    const int per_seq = p.Hkv * p.plan.tiles_per_unit, resident = (int)gridDim.x;
+    const int L = in ? visible_len(p, lane) : 0;
+    const int t = in ? ((L + kKeys - 1) / kKeys + (p.N + kKeys - 1) / kKeys + kRound - 1) / kRound : 0;    // rounds
+    const int total = __reduce_add_sync(all, t), longest = __reduce_max_sync(all, t);
+    // lane k tries the k-th candidate for T, from the lower bound on (two rounds, 64 parts an item); the longest sequence
+    // whole always fits, as there are no more items than CTAs
+    const int bound = max(max((total * per_seq + resident - 1) / resident, (longest + 63) / 64), 2);
+    const int T = bound + lane * max(1, bound / 16);
+    int units = 0;
+    for (int j = 0; j < p.B; ++j) units += (__shfl_sync(all, t, j) + T - 1) / T;
+    const int best = min(longest, (int)__reduce_min_sync(all, units * per_seq <= resident ? T : 0x7FFFFFFF));
+    const int n = in ? (t + best - 1) / best : 0;
+    int end = n;                                            // ranges up to and with this sequence, per item
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int before = __shfl_up_sync(all, end, o);
+        if (lane >= o) end += before;
+    }
+    if (leave && in) {
+        p.left[lane] = n;
+        p.left[p.left_off + lane] = (end - n) * per_seq;
+    }
+    u.b = min(__popc(__ballot_sync(all, in && end * per_seq <= w)), p.B - 1);
+    u.L = __shfl_sync(all, L, u.b);
+    u.nsplit = __shfl_sync(all, n, u.b);
+    const int r = w - __shfl_sync(all, end - n, u.b) * per_seq;
+    u.split = r / per_seq;
+    const int item = r - u.split * per_seq;
+    u.c = item / p.plan.tiles_per_unit;
+    u.row0 = item % p.plan.tiles_per_unit;
+    u.slot = w;
+    return w < __shfl_sync(all, end, 31) * per_seq;
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCKS) attn_paged_rows_kernel(RowsParams p) {
+    using T = RowsGeo<D, NT>;
+    constexpr int KS = D / 16;              // k-steps of the product with K
+    constexpr int MTL = T::MTILES, WARPS = T::WARPS, ST = T::STAGES;
+    constexpr int CH = D / 8, LANE_ROWS = 32 / CH;             // 16-byte pieces of a row; rows a copy of the warp takes
+    extern __shared__ __align__(128) unsigned char smem[];
+
+    if (p.slots > 0) let_successor_start();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int i8 = lane >> 2, j4 = lane & 3;
+    const int N = p.N, G = p.G, R = p.R;
+    Unit u;
+    if (p.plan.balanced == 3) {
+        wait_for_predecessor();
+        if (!unit_by_length<WARPS>(p, blockIdx.x, lane, blockIdx.x == 0 && warp == 0, u)) return;
+    } else {
+        int item;
+        plan_decode(p.plan, blockIdx.x, item, u.split, u.nsplit, u.slot);
+        const int pair = item / p.plan.tiles_per_unit;   // b * Hkv + c
+        u.row0 = item % p.plan.tiles_per_unit;
+        u.b = pair / p.Hkv;
+        u.c = pair % p.Hkv;
+        wait_for_predecessor();
+        u.L = visible_len(p, u.b);
+    }
+    u.row0 *= T::ROWS;
+    const int b = u.b, c = u.c, row0 = u.row0, L = u.L;
+    if (tid == 0 && p.status) {
+        const int given = p.seq_lens[b];
+        if (given < 0 || given > p.Lmax) atomicOr((unsigned*)p.status, GSD_DEV_BAD_SEQ_LEN);
+    }
+    // Key tiles of 16: the prefix, then the draft block.  The CTA has [t_begin, t_end) of them, a warp every WARPS-th.
+    const int nPT = (L + kKeys - 1) / kKeys, nT = nPT + (N + kKeys - 1) / kKeys;
+    const int per = ((nT + WARPS - 1) / WARPS + u.nsplit - 1) / u.nsplit * WARPS;
+    const int t_begin = min(u.split * per, nT), t_end = min(t_begin + per, nT);
+    const int first = t_begin + warp;
+    const int n_tiles = max(0, (t_end - first + WARPS - 1) / WARPS);
+
+    // ---- the ring: K and V tiles of 16 rows, 16-byte pieces swizzled by the row
+    const uint32_t ring = smem_u32(smem) + warp * (ST * 2 * T::TILE);
+    const size_t row_elems = (size_t)p.Hkv * D;
+    const int32_t* table = p.pages.table + (size_t)b * p.pages.max_pages;
+    // the pages of the warp's tiles i0 + lane; -1: none (draft tiles, no such tile, no such page)
+    auto find_pages = [&](int i0) -> int {
+        const int key = (first + (i0 + lane) * WARPS) * kKeys;
+        if (i0 + lane >= n_tiles || key >= L || !GSD_IN_BOUNDS(key >> p.pages.page_log2 < p.pages.max_pages, p.status)) return -1;
+        const int page = table[key >> p.pages.page_log2];
+        if ((unsigned)page < (unsigned)p.pages.num_pages) return page;
+        if (p.status) atomicOr((unsigned*)p.status, GSD_DEV_BAD_PAGE);
+        return -1;
+    };
+    const int my_row = lane / CH, my_piece = lane % CH;
+    auto issue = [&](int i, uint32_t stage, int pages) {
+        const int t = first + i * WARPS;
+        const bool draft = t >= nPT;
+        const int key0 = (draft ? t - nPT : t) * kKeys;
+        const int page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
+        const int rows = draft ? N - key0 : page < 0 ? 0 : L - key0;         // of the tile that are read
+        const size_t row = draft ? (size_t)b * N + key0 : ((size_t)max(page, 0) << p.pages.page_log2) + (key0 & ((1 << p.pages.page_log2) - 1));
+        const size_t at = (row + my_row) * row_elems + (size_t)c * D + my_piece * 8;
+        const __nv_bfloat16* k = (draft ? p.draft_k : p.k_pages) + at;
+        const __nv_bfloat16* v = (draft ? p.draft_v : p.v_pages) + at;
+#pragma unroll
+        for (int x = 0; x < kKeys / LANE_ROWS; ++x) {
+            const int r = x * LANE_ROWS + my_row;
+            const uint32_t off = (uint32_t)(r * (D * 2) + ((my_piece ^ (r & 7)) << 4));
+            const int bytes = r < rows ? 16 : 0;
+            const size_t step = r < rows ? (size_t)(x * LANE_ROWS) * row_elems : 0;
+            cp_async16(stage + off, r < rows ? k + step : p.k_pages, bytes);
+            cp_async16(stage + T::TILE + off, r < rows ? v + step : p.v_pages, bytes);
+        }
+    };
+    int pages = find_pages(0), pages_next = find_pages(32);
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s) {
+        if (s < n_tiles) issue(s, ring + s * (2 * T::TILE), pages);
+        cp_async_commit();
+    }
+
+    // ---- the query rows as fragments (rows are columns of the products): a warp for every eight rows puts them where all
+    // warps find them
+    const uint32_t q_at = smem_u32(smem) + T::Q_AT + lane * 8;
+#pragma unroll
+    for (int nt = warp; nt < NT; nt += WARPS) {
+        const int row = row0 + nt * 8 + i8;
+        const bool in = row < R;
+        const int rr = in ? row : 0;
+        const __nv_bfloat16* q = p.q + (((size_t)b * N + rr / G) * p.Hq + c * G + rr % G) * D + 2 * j4;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const uint32_t lo = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16) : 0u, hi = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16 + 8) : 0u;
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(q_at + (nt * KS + ks) * 256), "r"(lo), "r"(hi) : "memory");
+        }
+    }
+    __syncthreads();
+    uint2 qf[NT == 1 ? KS : 1];
+    if (NT == 1) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[NT == 1 ? ks : 0] = lds64(q_at + ks * 256);
+    }
+
+    float o[NT][MTL][4];                    // columns 16 mt + i8 and the one 8 behind it, of rows 8 nt + 2 j4 + {0, 1}
+    float m_run[NT][2], l_run[NT][2];       // l: the lane's own keys
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int mt = 0; mt < MTL; ++mt) o[nt][mt][0] = o[nt][mt][1] = o[nt][mt][2] = o[nt][mt][3] = 0.f;
+        m_run[nt][0] = m_run[nt][1] = -CUDART_INF_F;
+        l_run[nt][0] = l_run[nt][1] = 0.f;
+    }
+    // where the lane's rows of the matrices start: K keys (lane & 15), pieces + (lane >> 4); V keys (lane & 7) + 8 (lane >> 4)
+    const int k_row = lane & 15, v_row = (lane & 7) + ((lane >> 4) << 3);
+    uint32_t stage = ring, fill = ring + (ST - 1) * (2 * T::TILE);
+    const uint32_t ring_end = ring + ST * (2 * T::TILE);
+#pragma unroll 1
+    for (int i = 0; i < n_tiles; ++i) {
+        const int ahead = i + ST - 1;
+        if ((ahead & 31) == 0) {
+            pages = pages_next;
+            pages_next = find_pages(ahead + 32);
+        }
+        if (ahead < n_tiles) issue(ahead, fill, pages);
+        cp_async_commit();
+        fill = stage;
+        cp_async_wait<ST - 1>();
+        __syncwarp();
+        const uint32_t sk = stage, sv = stage + T::TILE;
+        stage += 2 * T::TILE;
+        if (stage == ring_end) stage = ring;
+
+        // S^T = K Q^T: 16 keys (i8, i8 + 8) x 8 rows; two chains at least
+        constexpr int CHAINS = NT == 1 ? 2 : 1;
+        float s[NT][4], s1[CHAINS][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[nt][e] = s1[0][e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            uint32_t a[4];
+            ldmatrix_x4(a, sk + k_row * (D * 2) + (((ks * 2 + (lane >> 4)) ^ (k_row & 7)) << 4));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const uint2 q = NT == 1 ? qf[NT == 1 ? ks : 0] : lds64(q_at + (nt * KS + ks) * 256);
+                mma_bf16(NT == 1 && (ks & 1) ? s1[0] : s[nt], a, q.x, q.y);
+            }
+        }
+        if (NT == 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[0][e] += s1[0][e];
+        }
+        // ---- in log2 units, hidden ones -inf
+        const int t = first + i * WARPS;
+        bool raise = false;
+        if (t >= nPT) {
+            const int key0 = (t - nPT) * kKeys;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int row = row0 + nt * 8 + 2 * j4 + e;
+                    uint32_t w = row < R ? p.mask[((size_t)b * N + row / G) * p.W + (key0 >> 5)] >> (key0 & 16) : 0u;
+                    if (N - key0 < kKeys) w &= (1u << (N - key0)) - 1u;
+                    s[nt][e] = (w >> i8) & 1u ? s[nt][e] * p.scale_log2 : -CUDART_INF_F;
+                    s[nt][e + 2] = (w >> (i8 + 8)) & 1u ? s[nt][e + 2] * p.scale_log2 : -CUDART_INF_F;
+                }
+        } else {
+            const int key = t * kKeys + i8;
+            const bool lo = key < L, hi = key + 8 < L;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    s[nt][e] = lo ? s[nt][e] * p.scale_log2 : -CUDART_INF_F;
+                    s[nt][e + 2] = hi ? s[nt][e + 2] * p.scale_log2 : -CUDART_INF_F;
+                }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) raise |= fmaxf(s[nt][e], s[nt][e + 2]) > m_run[nt][e] + kLag;
+        if (__any_sync(0xFFFFFFFFu, raise)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float a[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(s[nt][e], s[nt][e + 2]);
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
+                    const float m_new = fmaxf(m_run[nt][e], mx), m_use = m_new == -CUDART_INF_F ? 0.f : m_new;   // (nothing visible yet)
+                    a[e] = fast_exp2(m_run[nt][e] - m_use);
+                    m_run[nt][e] = m_new;
+                    l_run[nt][e] *= a[e];
+                }
+#pragma unroll
+                for (int mt = 0; mt < MTL; ++mt) {
+                    o[nt][mt][0] *= a[0]; o[nt][mt][2] *= a[0];
+                    o[nt][mt][1] *= a[1]; o[nt][mt][3] *= a[1];
+                }
+            }
+        }
+        uint32_t pf[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float m_use = m_run[nt][e] == -CUDART_INF_F ? 0.f : m_run[nt][e];
+                s[nt][e] = fast_exp2(s[nt][e] - m_use);
+                s[nt][e + 2] = fast_exp2(s[nt][e + 2] - m_use);
+                l_run[nt][e] += s[nt][e] + s[nt][e + 2];
+            }
+            pf[nt][0] = transpose8(pack_bf16(s[nt][0], s[nt][1]));
+            pf[nt][1] = transpose8(pack_bf16(s[nt][2], s[nt][3]));
+        }
+        // O^T += V^T P^T
+#pragma unroll
+        for (int mt = 0; mt < MTL; ++mt) {
+            uint32_t a[4];
+            ldmatrix_x4_trans(a, sv + v_row * (D * 2) + (((mt * 2 + ((lane >> 3) & 1)) ^ (v_row & 7)) << 4));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][mt], a, pf[nt][0], pf[nt][1]);
+        }
+        __syncwarp();                       // the stage has been read: a copy may take its place
+    }
+    cp_async_wait<0>();
+
+    // ---- the warps' results meet in the memory of the rings
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) l_run[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l_run[nt][e], x);
+    float* const part = reinterpret_cast<float*>(smem);
+    auto part_of = [&](int w, int nt) { return part + (w * NT + nt) * (T::VALUES * 32); };
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        float* at = part_of(warp, nt);
+        // (swizzled so that neither these stores nor the loads below conflict)
+#pragma unroll
+        for (int mt = 0; mt < MTL; ++mt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) at[(mt * 4 + e) * 32 + (lane ^ (e << 2))] = o[nt][mt][e];
+        if (i8 == 0) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                at[MTL * 128 + 2 * j4 + e] = m_run[nt][e];
+                at[MTL * 128 + 8 + 2 * j4 + e] = l_run[nt][e];
+            }
+        }
+    }
+    __syncthreads();
+    // a thread takes four columns of a row
+#pragma unroll 1
+    for (int x = tid; x < NT * 8 * (D / 4); x += T::THREADS) {
+        const int r8 = x & 7, quad = (x >> 3) % (D / 4), nt = (x >> 3) / (D / 4);
+        const int row = row0 + nt * 8 + r8;
+        if (row >= R) continue;
+        float w[WARPS], m = -CUDART_INF_F, l = 0.f;
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) {
+            w[k] = part_of(k, nt)[MTL * 128 + r8];
+            m = fmaxf(m, w[k]);
+        }
+        const float m_use = m == -CUDART_INF_F ? 0.f : m;
+        float r[4] = {0.f, 0.f, 0.f, 0.f};
+        const int col = quad * 4, e = ((col >> 3) & 1) * 2 + (r8 & 1), at = ((col >> 4) * 4 + e) * 32;
+#pragma unroll
+        for (int k = 0; k < WARPS; ++k) {
+            const float wk = fast_exp2(w[k] - m_use);
+            l += wk * part_of(k, nt)[MTL * 128 + 8 + r8];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) r[y] += wk * part_of(k, nt)[at + ((((col & 7) + y) * 4 + (r8 >> 1)) ^ (e << 2))];
+        }
+        if (u.nsplit == 1) {
+            if (!GSD_IN_BOUNDS(b < p.B && c < p.Hkv && row < p.R, p.status)) continue;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            *reinterpret_cast<uint2*>(p.out + (((size_t)b * N + row / G) * p.Hq + c * G + row % G) * D + col) =
+                make_uint2(pack_bf16(r[0] * inv, r[1] * inv), pack_bf16(r[2] * inv, r[3] * inv));
+        } else {
+            if (!GSD_IN_BOUNDS(u.slot >= 0 && u.slot < p.slots, p.status)) continue;
+            *reinterpret_cast<float4*>(p.part_o + (((size_t)u.slot * (D / 4) + quad) * 64 + nt * 8 + r8) * 4) = make_float4(r[0], r[1], r[2], r[3]);
+            if (quad == 0) *reinterpret_cast<float2*>(p.part_ml + ((size_t)u.slot * 64 + nt * 8 + r8) * 2) = make_float2(m, l);
+        }
+    }
+}
+
+template <int D, int NT>
+int launch_t(const AttnArgs& a) {
+    RowsParams p;
+    p.q = (const __nv_bfloat16*)a.q; p.draft_k = (const __nv_bfloat16*)a.draft_k; p.draft_v = (const __nv_bfloat16*)a.draft_v;
+    p.k_pages = (const __nv_bfloat16*)a.k_cache; p.v_pages = (const __nv_bfloat16*)a.v_cache; p.pages = a.pages;
+    p.mask = a.mask; p.seq_lens = a.seq_lens; p.out = (__nv_bfloat16*)a.out; p.status = a.status;
+    p.B = a.B; p.N = a.N; p.Hq = a.Hq; p.Hkv = a.Hkv; p.Lmax = a.Lmax; p.G = a.G; p.W = a.W; p.R = a.N * a.G;
+    p.scale_log2 = a.scale_log2; p.plan = a.plan.dev; p.slots = a.plan.slots;
+    p.part_o = (float*)a.workspace;
+    p.part_ml = (float*)((char*)a.workspace + plan_part_o_bytes(a.plan, a.D));
+    p.left = a.plan.dev.balanced == 3 ? plan_left_table(a.plan, a.D, a.workspace) : nullptr;
+    p.left_off = (int)(align_up((size_t)a.B * sizeof(int), 256) / sizeof(int));
+    constexpr int smem = RowsGeo<D, NT>::SMEM;
+    {
+        static bool done[64] = {};   // per template instance: the opt-in sticks per device
+        int dev = 0;
+        GSD_CUDA_TRY(cudaGetDevice(&dev));
+        if (dev < 0 || dev >= 64 || !done[dev]) {
+            GSD_CUDA_TRY(cudaFuncSetAttribute(attn_paged_rows_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+            if (dev >= 0 && dev < 64) done[dev] = true;
+        }
+    }
+    GSD_CUDA_TRY(launch_dependent(attn_paged_rows_kernel<D, NT>, dim3(a.plan.ctas), dim3(RowsGeo<D, NT>::THREADS), smem, a.stream, p));
+    return GSD_OK;
+}
+
+}  // namespace
+
+// Stacked rows of an item: as few items as 32 rows each (64 at D = 64, whose accumulators are half as wide) allow, with the row
+// groups shared out evenly.
+int attn_paged_rows(int R, int D) {
+    const int most = D == 64 ? 64 : 32, items = (R + most - 1) / most, groups = (R + 7) / 8;
+    const int even = (groups + items - 1) / items;
+    return 8 * (even > 4 ? (even + 1) / 2 * 2 : even);
+}
+int attn_paged_rows_resident(int R, int D) { return D == 64 && attn_paged_rows(R, D) <= 16 ? 2 : 1; }
+
+int launch_attn_paged_rows(const AttnArgs& a) {
+    switch (a.plan.rows_per_item * 1000 + a.D) {
+        case 8128: return launch_t<128, 1>(a);
+        case 16128: return launch_t<128, 2>(a);
+        case 24128: return launch_t<128, 3>(a);
+        case 32128: return launch_t<128, 4>(a);
+        case 8064: return launch_t<64, 1>(a);
+        case 16064: return launch_t<64, 2>(a);
+        case 24064: return launch_t<64, 3>(a);
+        case 32064: return launch_t<64, 4>(a);
+        case 48064: return launch_t<64, 6>(a);
+        case 64064: return launch_t<64, 8>(a);
+    }
+    return GSD_ERR_BAD_SHAPE;
+}
+
+}  // namespace gsd
