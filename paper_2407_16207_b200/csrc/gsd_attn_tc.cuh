@@ -211,6 +211,13 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
         ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar,
+                                            int c0, int c1, int c2, int c3, int c4) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
+}
+
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -310,6 +317,10 @@ constexpr uint64_t kDescBase = (1ull << 46) | (2ull << 61);   // descriptor vers
 constexpr uint32_t kDescHi = (uint32_t)((kDescBase | ((uint64_t)(1024 >> 4) << 32)) >> 32);
 __device__ __forceinline__ uint32_t desc_lo_kmajor(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | (1u << 16); }
 __device__ __forceinline__ uint32_t desc_lo_mnmajor(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | ((HALF_BYTES >> 4) << 16); }
+// K and V tiles at HD = 128 from pages (PAGED): the two 64-column blocks side by side in every group of 8 rows, so that one
+// copy brings both of them: 2048 bytes between groups, 1024 between blocks.
+constexpr uint32_t kDescHiPaged = (uint32_t)((kDescBase | ((uint64_t)(2048 >> 4) << 32)) >> 32);
+__device__ __forceinline__ uint32_t desc_lo_mnmajor_paged(uint32_t addr) { return ((addr & 0x3FFFFu) >> 4) | ((1024u >> 4) << 16); }
 // instruction descriptors: bf16 x bf16 -> fp32, M = 128; N = 128 keys
 constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 // O += P V: N = head dimension, B (= V) is MN-major
@@ -339,6 +350,21 @@ __device__ __forceinline__ void tc_qk(uint32_t d_tmem, uint32_t alo, uint32_t bl
 #undef GSD_QK_HEAD
 #undef GSD_QK_STEP
 }
+// The same with such a K tile.
+__device__ __forceinline__ void tc_qk_paged(uint32_t d_tmem, uint32_t alo, uint32_t blo) {
+#define GSD_QK_STEP(AOFF, BOFF, P)                                                  \
+    " add.u32 al, %1, " #AOFF ";\n add.u32 bl, %2, " #BOFF ";\n"                     \
+    " mov.b64 a, {al, %3};\n mov.b64 b, {bl, %5};\n"                                \
+    " @q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, " #P ";\n"
+    asm volatile(
+        "{\n .reg .pred q, pt, pf;\n .reg .b64 a, b;\n .reg .b32 al, bl;\n"
+        " elect.sync _|q, 0xffffffff;\n"
+        " setp.eq.u32 pt, %4, %4;\n setp.ne.u32 pf, %4, %4;\n"
+        GSD_QK_STEP(0, 0, pf) GSD_QK_STEP(2, 2, pt) GSD_QK_STEP(4, 4, pt) GSD_QK_STEP(6, 6, pt)
+        GSD_QK_STEP(1024, 64, pt) GSD_QK_STEP(1026, 66, pt) GSD_QK_STEP(1028, 68, pt) GSD_QK_STEP(1030, 70, pt) "}\n"
+        ::"r"(d_tmem), "r"(alo), "r"(blo), "r"(kDescHi), "r"(kIdescQK), "r"(kDescHiPaged) : "memory");
+#undef GSD_QK_STEP
+}
 // O (+)= P V for four k-steps of 16 keys: A = 8 TMEM columns of bf16 pairs per step, B = the
 // MN-major V tile (2048 bytes per 16 keys).  `accum_first` = 0 makes the first step overwrite O.
 template <int HD>
@@ -353,6 +379,20 @@ __device__ __forceinline__ void tc_pv4(uint32_t d_tmem, uint32_t a_tmem, uint32_
         GSD_PV_STEP(0, 0, p0) GSD_PV_STEP(8, 128, pt) GSD_PV_STEP(16, 256, pt) GSD_PV_STEP(24, 384, pt)
         "}\n"
         ::"r"(d_tmem), "r"(a_tmem), "r"(blo), "r"(kDescHi), "r"(kIdescPV<HD>), "r"(accum_first) : "memory");
+#undef GSD_PV_STEP
+}
+// The same with such a V tile: 4096 bytes per 16 keys.
+__device__ __forceinline__ void tc_pv4_paged(uint32_t d_tmem, uint32_t a_tmem, uint32_t blo, uint32_t accum_first) {
+#define GSD_PV_STEP(ACOL, BOFF, P)                                                  \
+    " add.u32 at, %1, " #ACOL ";\n add.u32 bl, %2, " #BOFF ";\n mov.b64 b, {bl, %3};\n" \
+    " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [at], b, %4, " #P ";\n"
+    asm volatile(
+        "{\n .reg .pred q, pt, p0;\n .reg .b64 b;\n .reg .b32 at, bl;\n"
+        " elect.sync _|q, 0xffffffff;\n"
+        " setp.eq.u32 pt, %4, %4;\n setp.ne.u32 p0, %5, 0;\n"
+        GSD_PV_STEP(0, 0, p0) GSD_PV_STEP(8, 256, pt) GSD_PV_STEP(16, 512, pt) GSD_PV_STEP(24, 768, pt)
+        "}\n"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(blo), "r"(kDescHiPaged), "r"(kIdescPV<128>), "r"(accum_first) : "memory");
 #undef GSD_PV_STEP
 }
 
@@ -625,12 +665,12 @@ __device__ __forceinline__ bool order_by_length(const TcParams& p, int* s_len, i
     return __syncthreads_or(tid < B && mine != s_len[0]) != 0;
 }
 
-// A cache in pages (PAGED): a prefix tile is 128 / box pieces of `box` rows, a piece in one page, box = min(page, 128); a lane of the
-// producer warp copies a 64-column block of a piece.  The page is the outermost coordinate of the copy, so that an entry
-// which names no page could not reach memory outside the pool even unlooked at.  The rows of a page behind the sequence's end
-// may be anything, so the piece that holds the end is copied as the box that ends there: it starts before the page's (or the
-// piece's) first row, and the rows before row 0 come back as zeros.  Its visible keys are its LAST ones; pieces behind it, and those of
-// a page that the table does not name, are copied from behind the page's last row: zeros.
+// A cache in pages (PAGED): a prefix tile is 128 / box pieces of `box` rows, a piece in one page, box = min(page, 128); each lane of the
+// producer warp copies a part of the tile.  The page is the outermost coordinate of the copy, so that an entry which names no
+// page could not reach memory outside the pool even unlooked at.  The rows of a page behind the sequence's end may be
+// anything, so the piece that holds the end is copied as the rows up to the end: it starts before the page's (or the piece's)
+// first row, and the rows before row 0 come back as zeros.  Its visible keys are its LAST ones; pieces behind it, and those of a
+// page that the table does not name, are copied from behind the page's last row: zeros.
 struct PieceAt {
     int row, page;
 };
@@ -648,6 +688,16 @@ __device__ __forceinline__ PieceAt piece_at(const TcParams& p, int b, int L, int
     }
     return at;
 }
+// At HD = 128 a tile of 128 visible rows takes one copy a piece, for both column blocks of it (five dimensions: 64 columns,
+// row % 8, column block, row / 8, page), and the last tile of a prefix and draft tiles, which may begin at any row, one for every 8
+// rows.  With a copy for each block, pages of 16 kept the copy engine busy: 4 x 40 heads, N 128, L 1024-4096 81.5 us, now KKK;
+// 8 x 64/8, N 256, L 4096 295, now KKK.
+template <bool PAGED>
+struct PagedMaps {};
+template <>
+struct PagedMaps<true> {
+    CUtensorMap k, v;
+};
 // the lowest n bits (any n)
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
 
@@ -659,7 +709,7 @@ template <int HD, int PLAN, bool LONG_MASK, bool PAGED>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_dk,
-               const __grid_constant__ CUtensorMap tm_dv, const TcParams p) {
+               const __grid_constant__ CUtensorMap tm_dv, const __grid_constant__ PagedMaps<PAGED> tm_pages, const TcParams p) {
     using T = Geo<HD>;
     constexpr uint32_t TILE_BYTES = T::TILE_BYTES;
     constexpr int ST = T::ST;
@@ -692,6 +742,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         // 363, L 228: 142 and 162 - one of 1 x 8/1, N 27, L 97: 10.3 and 9.8).
         if (p.slots > 0) let_successor_start();
         // the first copy through a tensor map would otherwise fetch it from memory first
+        if constexpr (PAGED) { prefetch_map(&tm_pages.k); prefetch_map(&tm_pages.v); }
         prefetch_map(&tm_q); prefetch_map(&tm_k); prefetch_map(&tm_v); prefetch_map(&tm_dk); prefetch_map(&tm_dv);
         s_wait.abort = 0;
         s_wait.limit_ns = p.wait_limit_ns;
@@ -783,21 +834,38 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 tma_load_4d(sQ + i * TILE_BYTES + h * HALF_BYTES, &tm_q, bar(BAR_Q_FULL), h * 64, u.c * G, (u.row0 + i * RT) / G, u.b);
     };
     // PAGED, by the whole warp: where this lane's piece of a key tile lies, and the copies of the tile.
+    constexpr bool SIDE = PAGED && T::BLOCKS == 2;       // column blocks side by side
     auto piece_of = [&](const UnitInfo& u, int idx) -> PieceAt {
-        const int piece = lane / T::BLOCKS, t = u.t_begin + idx;
-        if (t >= u.nPT || (piece << p.box_log2) >= BN) return PieceAt{0, 0};
-        return piece_at(p, u.b, u.L, t * BN + (piece << p.box_log2));
+        const int t = u.t_begin + idx;
+        int off = lane / T::BLOCKS << p.box_log2;        // the lane's rows of the tile
+        if (SIDE) off = t < u.L / BN ? lane << p.box_log2 : lane * 8;
+        if (t >= u.nPT || off >= BN) return PieceAt{0, 0};
+        const int box = 1 << p.box_log2, in_piece = off & (box - 1);
+        PieceAt at = piece_at(p, u.b, u.L, t * BN + off - in_piece);
+        at.row += in_piece;
+        return at;
     };
     auto load_pieces = [&](const UnitInfo& u, int idx, int n, const PieceAt& at, bool v) {
-        const int t = u.t_begin + idx, h = lane % T::BLOCKS, piece = lane / T::BLOCKS;
+        const int t = u.t_begin + idx;
         const uint32_t full = bar((v ? BAR_V_FULL : BAR_K_FULL) + n % ST);
-        const uint32_t dst = (v ? sV : sK) + (n % ST) * TILE_BYTES + h * HALF_BYTES;
+        const uint32_t dst = (v ? sV : sK) + (n % ST) * TILE_BYTES;
         if (lane == 0) mbar_expect_tx(full, TILE_BYTES);
         if (!v && p.withhold_first_k && n == 0) return;  // (test hook: the bytes announced above never arrive)
-        if (t >= u.nPT) {
-            if (piece == 0) tma_load_4d(dst, v ? &tm_dv : &tm_dk, full, h * 64, u.c, tile_info(t, u.nPT, u.L, u.live).key0, u.b);
-        } else if ((piece << p.box_log2) < BN) {
-            tma_load_4d(dst + ((uint32_t)piece << (p.box_log2 + 7)), v ? &tm_v : &tm_k, full, h * 64, u.c, at.row, at.page);
+        if constexpr (SIDE) {
+            if (t < u.L / BN) {
+                if ((lane << p.box_log2) < BN)
+                    tma_load_5d(dst + ((uint32_t)lane << (p.box_log2 + 8)), v ? &tm_pages.v : &tm_pages.k, full, 0, 0, u.c * 2, at.row >> 3, at.page);
+            } else if (lane < BN / 8) {
+                if (t < u.nPT) tma_load_4d(dst + lane * 2048, v ? &tm_v : &tm_k, full, 0, at.row, u.c * 2, at.page);
+                else tma_load_4d(dst + lane * 2048, v ? &tm_dv : &tm_dk, full, 0, tile_info(t, u.nPT, u.L, u.live).key0 + lane * 8, u.c * 2, u.b);
+            }
+        } else {
+            const int h = lane % T::BLOCKS, piece = lane / T::BLOCKS;
+            if (t >= u.nPT) {
+                if (piece == 0) tma_load_4d(dst + h * HALF_BYTES, v ? &tm_dv : &tm_dk, full, h * 64, u.c, tile_info(t, u.nPT, u.L, u.live).key0, u.b);
+            } else if ((piece << p.box_log2) < BN) {
+                tma_load_4d(dst + h * HALF_BYTES + ((uint32_t)piece << (p.box_log2 + 7)), v ? &tm_v : &tm_k, full, h * 64, u.c, at.row, at.page);
+            }
         }
         __syncwarp();
     };
@@ -1024,7 +1092,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     if (!(ok = wait(BAR_S_FREE + s_owner, (uint32_t)((s_owner ? jq1 : jq0) - 1) & 1u))) break;
                 }
                 tc_fence_after();
-                tc_qk<HD>(tmem + (i ? T::COL_S1 : T::COL_S0), (two && i) ? qlo1 : qlo0, klo0 + (uint32_t)st * (TILE_BYTES >> 4));
+                if constexpr (SIDE)
+                    tc_qk_paged(tmem + (i ? T::COL_S1 : T::COL_S0), (two && i) ? qlo1 : qlo0, klo0 + (uint32_t)st * (TILE_BYTES >> 4));
+                else
+                    tc_qk<HD>(tmem + (i ? T::COL_S1 : T::COL_S0), (two && i) ? qlo1 : qlo0, klo0 + (uint32_t)st * (TILE_BYTES >> 4));
                 tc_commit(bar(BAR_S_FULL + i));
                 if (!two || i == 1) tc_commit(bar(BAR_K_EMPTY + st));
                 if (k == njobs - 1) tc_commit(bar(BAR_Q_EMPTY));   // every QK^T of the unit is issued
@@ -1050,7 +1121,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         int jp0 = 0, jp1 = 0;     // jobs issued per stream so far (phase of P_READY / P_FREE)
         bool ok = true;
         auto wait = [&](int b, uint32_t par) -> bool { return mbar_wait_warp(bar(b), par, abort_flag, p.status); };
-        const uint32_t vlo0 = desc_lo_mnmajor(sV);      // (stage st: + st * TILE_BYTES / 16)
+        const uint32_t vlo0 = SIDE ? desc_lo_mnmajor_paged(sV) : desc_lo_mnmajor(sV);      // (stage st: + st * TILE_BYTES / 16)
         for (int it = 0; it < n_my && ok; ++it) {
             const UnitInfo u = unit_of(it);
             if (u.ntiles == 0) continue;
@@ -1073,10 +1144,12 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                     if (!(ok = wait(BAR_O_FREE + i, (uint32_t)((i ? au1 : au) - 1) & 1u))) break;
                 }
                 tc_fence_after();
-                tc_pv4<HD>(tO, tP, vlo, first ? 0u : 1u);
+                if constexpr (SIDE) tc_pv4_paged(tO, tP, vlo, first ? 0u : 1u);
+                else tc_pv4<HD>(tO, tP, vlo, first ? 0u : 1u);
                 if (!(ok = wait(BAR_P_READY2 + i, par))) break;
                 tc_fence_after();
-                tc_pv4<HD>(tO, tP + 32, vlo + 4 * 128, 1u);
+                if constexpr (SIDE) tc_pv4_paged(tO, tP + 32, vlo + 4 * 256, 1u);
+                else tc_pv4<HD>(tO, tP + 32, vlo + 4 * 128, 1u);
                 tc_commit(bar(BAR_P_FREE + i));
                 if (!two || i == 1) tc_commit(bar(BAR_V_EMPTY + st));
                 if (k + 2 >= njobs) tc_commit(bar(BAR_O_DONE + i));   // the stream's last job of the unit
@@ -1431,15 +1504,11 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// [d3][d2][d1][D] bf16 tensor; box = 64 columns x box1 x box2 x 1, 128-byte swizzle, zero fill
-int make_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t d1, uint64_t d2, uint64_t d3, uint32_t box1, uint32_t box2) {
+int encode_map(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return GSD_ERR_CUDA;
-    const cuuint64_t dims[4] = {(cuuint64_t)HD, d1, d2, d3};
-    const cuuint64_t strides[3] = {(cuuint64_t)HD * 2, (cuuint64_t)HD * 2 * d1, (cuuint64_t)HD * 2 * d1 * d2};
-    const cuuint32_t box[4] = {64, box1, box2, 1};
-    const cuuint32_t estr[4] = {1, 1, 1, 1};
-    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
@@ -1451,6 +1520,31 @@ int make_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t d1, uint64_
     return GSD_OK;
 }
 
+// [d3][d2][d1][D] bf16 tensor; box = 64 columns x box1 x box2 x 1, 128-byte swizzle, zero fill
+int make_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t d1, uint64_t d2, uint64_t d3, uint32_t box1, uint32_t box2) {
+    const cuuint64_t dims[4] = {(cuuint64_t)HD, d1, d2, d3};
+    const cuuint64_t strides[3] = {(cuuint64_t)HD * 2, (cuuint64_t)HD * 2 * d1, (cuuint64_t)HD * 2 * d1 * d2};
+    const cuuint32_t box[4] = {64, box1, box2, 1};
+    return encode_map(m, base, 4, dims, strides, box);
+}
+
+// [P][rows][Hkv][HD], 8 rows of a head from any row on, the column blocks one behind the other
+int make_group_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t Hkv, uint64_t rows, uint64_t P) {
+    const cuuint64_t row = HD * 2 * Hkv;
+    const cuuint64_t dims[4] = {64, rows, HD / 64 * Hkv, P};
+    const cuuint64_t strides[3] = {row, 128, rows * row};
+    const cuuint32_t box[4] = {64, 8, (cuuint32_t)(HD / 64), 1};
+    return encode_map(m, base, 4, dims, strides, box);
+}
+// Pages [P][page][Hkv][HD], a piece of one: box / 8 such groups
+int make_page_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t Hkv, uint64_t page, uint64_t P, uint32_t box) {
+    const cuuint64_t row = HD * 2 * Hkv;
+    const cuuint64_t dims[5] = {64, 8, HD / 64 * Hkv, page / 8, P};
+    const cuuint64_t strides[4] = {row, 128, 8 * row, page * row};
+    const cuuint32_t boxes[5] = {64, 8, (cuuint32_t)(HD / 64), box / 8, 1};
+    return encode_map(m, base, 5, dims, strides, boxes);
+}
+
 }  // namespace
 
 template <int HD, int PLAN, bool LONG_MASK, bool PAGED>
@@ -1459,12 +1553,30 @@ static int launch_tc(const AttnArgs& a) {
     CUtensorMap tq, tk, tv, tdk, tdv;
     int rc;
     if ((rc = make_map(&tq, a.q, HD, a.Hq, a.N, a.B, a.G, nodes)) != GSD_OK) return rc;
-    const int page = PAGED ? 1 << a.pages.page_log2 : 0, box = page < BN ? page : BN;
-    const uint64_t rows = PAGED ? page : a.Lmax, ranges = PAGED ? a.pages.num_pages : a.B;
-    if ((rc = make_map(&tk, a.k_cache, HD, a.Hkv, rows, ranges, 1, PAGED ? box : BN)) != GSD_OK) return rc;
-    if ((rc = make_map(&tv, a.v_cache, HD, a.Hkv, rows, ranges, 1, PAGED ? box : BN)) != GSD_OK) return rc;
-    if ((rc = make_map(&tdk, a.draft_k, HD, a.Hkv, a.N, a.B, 1, BN)) != GSD_OK) return rc;
-    if ((rc = make_map(&tdv, a.draft_v, HD, a.Hkv, a.N, a.B, 1, BN)) != GSD_OK) return rc;
+    PagedMaps<PAGED> pages;
+    if constexpr (PAGED) {
+        const int page = 1 << a.pages.page_log2, box = page < BN ? page : BN, P = a.pages.num_pages;
+        if constexpr (HD == 128) {
+            if ((rc = make_page_map(&pages.k, a.k_cache, HD, a.Hkv, page, P, box)) != GSD_OK) return rc;
+            if ((rc = make_page_map(&pages.v, a.v_cache, HD, a.Hkv, page, P, box)) != GSD_OK) return rc;
+            if ((rc = make_group_map(&tk, a.k_cache, HD, a.Hkv, page, P)) != GSD_OK) return rc;
+            if ((rc = make_group_map(&tv, a.v_cache, HD, a.Hkv, page, P)) != GSD_OK) return rc;
+            if ((rc = make_group_map(&tdk, a.draft_k, HD, a.Hkv, a.N, a.B)) != GSD_OK) return rc;
+            if ((rc = make_group_map(&tdv, a.draft_v, HD, a.Hkv, a.N, a.B)) != GSD_OK) return rc;
+        } else {
+            if ((rc = make_map(&tk, a.k_cache, HD, a.Hkv, page, P, 1, box)) != GSD_OK) return rc;
+            if ((rc = make_map(&tv, a.v_cache, HD, a.Hkv, page, P, 1, box)) != GSD_OK) return rc;
+            pages.k = tk;
+            pages.v = tv;
+        }
+    } else {
+        if ((rc = make_map(&tk, a.k_cache, HD, a.Hkv, a.Lmax, a.B, 1, BN)) != GSD_OK) return rc;
+        if ((rc = make_map(&tv, a.v_cache, HD, a.Hkv, a.Lmax, a.B, 1, BN)) != GSD_OK) return rc;
+    }
+    if constexpr (!PAGED || HD != 128) {
+        if ((rc = make_map(&tdk, a.draft_k, HD, a.Hkv, a.N, a.B, 1, BN)) != GSD_OK) return rc;
+        if ((rc = make_map(&tdv, a.draft_v, HD, a.Hkv, a.N, a.B, 1, BN)) != GSD_OK) return rc;
+    }
     TcParams p;
     p.mask = a.mask; p.seq_lens = a.seq_lens; p.out = (__nv_bfloat16*)a.out; p.status = a.status;
     p.out_by_32 = ((uintptr_t)a.out & 31u) == 0;
@@ -1524,7 +1636,7 @@ static int launch_tc(const AttnArgs& a) {
     const int part = PLAN == PLAN_FIXED || PLAN == PLAN_ORDERED ? (int)cfg.gridDim.x * kUnitTable : a.plan.ctas;
     for (p.work0 = 0; p.work0 < a.plan.ctas; p.work0 += part) {
         p.total_work = a.plan.ctas - p.work0 < part ? a.plan.ctas - p.work0 : part;
-        GSD_CUDA_TRY(cudaLaunchKernelEx(&cfg, attn_tc_kernel<HD, PLAN, LONG_MASK, PAGED>, tq, tk, tv, tdk, tdv, p));
+        GSD_CUDA_TRY(cudaLaunchKernelEx(&cfg, attn_tc_kernel<HD, PLAN, LONG_MASK, PAGED>, tq, tk, tv, tdk, tdv, pages, p));
     }
     return GSD_OK;
 }
