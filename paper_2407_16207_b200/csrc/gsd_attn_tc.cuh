@@ -690,8 +690,8 @@ __device__ __forceinline__ PieceAt piece_at(const TcParams& p, int b, int L, int
 }
 // At HD = 128 a tile of 128 visible rows takes one copy a piece, for both column blocks of it (five dimensions: 64 columns,
 // row % 8, column block, row / 8, page), and the last tile of a prefix and draft tiles, which may begin at any row, one for every 8
-// rows.  With a copy for each block, pages of 16 kept the copy engine busy: 4 x 40 heads, N 128, L 1024-4096 81.5 us, now KKK;
-// 8 x 64/8, N 256, L 4096 295, now KKK.
+// rows.  With a copy for each block, pages of 16 kept the copy engine busy: 4 x 40 heads, N 128, L 1024-4096 81.5 us, so 70.9, with a
+// producer warp each for K and V 57.9 (56 over a padded cache); 8 x 64/8, N 256, L 4096 295, 246 and 243 (237).
 template <bool PAGED>
 struct PagedMaps {};
 template <>
@@ -966,7 +966,44 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 
     if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    if (warp == 8) {
+    if (PAGED && (warp == 8 || warp == 10)) {
+        // ------------------------------------------------------------ TMA producers: Q and K, V
+        // A lane a part of a tile.  Pages of 16 take eight copies a tile, each a dozen instructions beside the softmax warps: two
+        // warps issue them, K and V each as soon as its slot is free.  Where a tile's parts lie is asked for a tile ahead.
+        const bool v = warp == 10;
+        const int full = v ? BAR_V_FULL : BAR_K_FULL, empty = v ? BAR_V_EMPTY : BAR_K_EMPTY;
+        int pos = 0;                    // tiles loaded so far (ring position)
+        int au = 0;                     // non-empty units so far
+        bool ok = true, q_pending = false;
+        for (int it = 0; it < n_my && ok; ++it) {
+            const UnitInfo u = unit_of(it);
+            if (u.ntiles == 0) continue;
+            const int begun = it == 0 ? max(0, min(ST, min(u.nPT - u.t_begin, u.ntiles))) : 0;    // on their way already
+            pos += begun;
+            PieceAt next = piece_of(u, begun);
+            if (!v && begun == 0) {
+                // Q of the previous unit is free once its last QK^T has completed
+                ok = mbar_wait_warp(bar(BAR_Q_EMPTY), (au & 1) ^ 1, abort_flag, p.status);
+                if (ok && lane == 0) load_q(u);
+            }
+            q_pending = !v && ok;
+            for (int t = begun; t < u.ntiles && ok; ++t) {
+                ok = mbar_wait_warp(bar(empty + pos % ST), (uint32_t)((pos / ST) & 1) ^ 1u, abort_flag, p.status);
+                if (!ok) break;
+                load_pieces(u, t, pos, next, v);
+                ++pos;
+                if (t + 1 < u.ntiles) next = piece_of(u, t + 1);
+            }
+            if (!ok && lane == 0) {
+                // gave up: let the copies already in flight land before the CTA retires
+                if (q_pending) mbar_wait_slow(bar(BAR_Q_FULL), au & 1, abort_flag, nullptr, true);
+                for (int t = max(0, pos - ST); t < pos; ++t)
+                    mbar_wait_slow(bar(full + t % ST), (t / ST) & 1, abort_flag, nullptr, true);
+            }
+            __syncwarp();
+            ++au;
+        }
+    } else if (warp == 8) {
         // ------------------------------------------------------------ TMA producer
         // Units with one row tile, where loads are the bound: K copies run one tile ahead of the V
         // copies.  K t + 1 only waits for the QK^T of tile t - 1, and its time to land passes while V t
@@ -978,46 +1015,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         int kc = pre, vc = pre;         // K and V tiles loaded so far (ring positions)
         int au = 0;                     // non-empty units so far
         bool ok = true, q_pending = pre > 0;
-        auto drain = [&]() {
-            // gave up: let the copies already in flight land before the CTA retires
-            if (q_pending) mbar_wait_slow(bar(BAR_Q_FULL), au & 1, abort_flag, nullptr, true);
-            for (int t = max(0, kc - ST); t < kc; ++t)
-                mbar_wait_slow(bar(BAR_K_FULL + t % ST), (t / ST) & 1, abort_flag, nullptr, true);
-            for (int t = max(0, vc - ST); t < vc; ++t)
-                mbar_wait_slow(bar(BAR_V_FULL + t % ST), (t / ST) & 1, abort_flag, nullptr, true);
-        };
         for (int it = 0; it < n_my && ok; ++it) {
             const UnitInfo u = unit_of(it);
             if (u.ntiles == 0) continue;
-            if (PAGED) {
-                // the same by the whole warp; where a tile's pieces lie is asked for before the wait for its slot
-                const bool begun = it == 0 && pre > 0;
-                if (!begun) {
-                    ok = mbar_wait_warp(bar(BAR_Q_EMPTY), (au & 1) ^ 1, abort_flag, p.status);
-                    if (ok) {
-                        if (lane == 0) load_q(u);
-                        q_pending = true;
-                    }
-                }
-                int kn = begun ? pre : 0, vn = kn;
-                PieceAt next = piece_of(u, kn);                  // of K tile kn
-                while (ok && vn < u.ntiles) {
-                    if (kn < u.ntiles && kn <= vn + (u.two ? 0 : 1)) {
-                        if (!(ok = mbar_wait_warp(bar(BAR_K_EMPTY + kc % ST), (uint32_t)((kc / ST) & 1) ^ 1u, abort_flag, p.status))) break;
-                        load_pieces(u, kn, kc, next, false);
-                        ++kn;
-                        ++kc;
-                        if (kn < u.ntiles) next = piece_of(u, kn);
-                    } else {
-                        const PieceAt at = piece_of(u, vn);
-                        if (!(ok = mbar_wait_warp(bar(BAR_V_EMPTY + vc % ST), (uint32_t)((vc / ST) & 1) ^ 1u, abort_flag, p.status))) break;
-                        load_pieces(u, vn, vc, at, true);
-                        ++vn;
-                        ++vc;
-                    }
-                }
-                if (!ok && lane == 0) drain();
-            } else if (lane == 0) {
+            if (lane == 0) {
                 const bool begun = it == 0 && pre > 0;
                 if (!begun) {
                     // Q of the previous unit is free once its last QK^T has completed
@@ -1052,7 +1053,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                         }
                     }
                 }
-                if (!ok) drain();
+                if (!ok) {
+                    // gave up: let the copies already in flight land before the CTA retires
+                    if (q_pending) mbar_wait_slow(bar(BAR_Q_FULL), au & 1, abort_flag, nullptr, true);
+                    for (int t = max(0, kc - ST); t < kc; ++t)
+                        mbar_wait_slow(bar(BAR_K_FULL + t % ST), (t / ST) & 1, abort_flag, nullptr, true);
+                    for (int t = max(0, vc - ST); t < vc; ++t)
+                        mbar_wait_slow(bar(BAR_V_FULL + t % ST), (t / ST) & 1, abort_flag, nullptr, true);
+                }
             }
             ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0) != 0;
             kc = __shfl_sync(0xFFFFFFFFu, kc, 0);
