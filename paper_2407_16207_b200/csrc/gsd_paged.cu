@@ -1,9 +1,11 @@
 // gsd_append_kv_paged and gsd_commit_kv_paged: bf16 K/V rows into a cache held in pages, behind the old end of every sequence
 // (the rows of a prompt, K rotated by position on the way; or the accepted path of a verification step).
 //
-// A thread has a chunk of 16 columns (gsd_rotary.cuh) of a row, of kHeads heads of K and the same of V; it asks for its pieces
-// of all of them and looks up the page and forms its sines and cosines while they come.  Rows from the first on whose page the
-// table does not name are dropped: every CTA looks through the entries up to its own last row's.
+// A CTA has a run of (row, kv head) places of a sequence, a thread a chunk of 16 columns of K and of V of several of them
+// (gsd_rotary.cuh).  While its first pieces come, the CTA looks up its rows' pages and forms their sines and cosines in shared
+// memory.  Rows from the first on whose page the table does not name are dropped: every CTA looks through the entries up to
+// its own last row's.  Bound by DRAM for prompts, by dependent trips to memory for accepted paths and short chunks, which go to one
+// cluster of CTAs per sequence, so that it can move the length on itself.
 #include "gsd_pages.cuh"
 #include "gsd_rotary.cuh"
 #include <initializer_list>
@@ -11,7 +13,7 @@
 namespace gsd {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kRotaryThreads;
 
 struct WriteArgs {
     uint16_t *k_pages, *v_pages;
@@ -25,23 +27,24 @@ struct WriteArgs {
     long long k_stride, v_stride;
     int B, M, Hkv, Lmax, Tcap;   // M: rows per sequence in k / v
     int page_log2, max_pages, num_pages;
-    int splits;                  // threads that share the heads of a row
+    int batches;                 // of a CTA (not of a path's)
 };
 
 enum Mode { APPEND, APPEND_CLUSTER, COMMIT };   // the rows of a grid, of one cluster per sequence; a path, one cluster per sequence
 
-// One CTA of a sequence's, or all of them together, take the rows; with a cluster CTA 0 moves the length on once all have
-// read the old one.
-template <int D, int kHeads, int MODE>
-__global__ void __launch_bounds__(kThreads) paged_write_kernel(WriteArgs a) {
-    constexpr int CH = D / 16, SLOTS = kThreads / CH;
+// With a cluster CTA 0 moves the length on once all of it have read the old one.
+template <int D, int kBatch, int MODE>
+__global__ void __launch_bounds__(kThreads, kRotaryBlocks) paged_write_kernel(const __grid_constant__ WriteArgs a) {
+    constexpr int CH = D / 16, SLOTS = kThreads / CH, ROWS = MODE == COMMIT ? GSD_MAX_NODES : rotary_tokens(D);
+    __shared__ AngleTable<D> s_angles[MODE == COMMIT ? 1 : ROWS];
+    __shared__ int s_page[ROWS];                                  // the pages of the CTA's rows
     __shared__ int s_src[MODE == COMMIT ? GSD_MAX_NODES : 1];     // source row of each new place
     __shared__ int s_tot[kThreads / 32];
     __shared__ int s_bad;                                         // first table entry that names no page
     let_successor_start();
     const int b = blockIdx.y, tid = threadIdx.x;
-    const bool leader = blockIdx.x == 0;
     if (tid == 0) s_bad = 0x7FFFFFFF;
+    __syncthreads();
     wait_for_predecessor();
     unsigned flags = 0;
     int L = a.seq_lens[b];
@@ -78,60 +81,63 @@ __global__ void __launch_bounds__(kThreads) paged_write_kernel(WriteArgs a) {
     if (n > a.Lmax - L) flags |= GSD_DEV_CACHE_FULL;
     n = min(n, a.Lmax - L);
 
-    const int32_t* row = a.table + (size_t)b * a.max_pages;
-    const int page = 1 << a.page_log2, first_entry = L >> a.page_log2;
-    const int stride = (int)gridDim.x * SLOTS, begin = (int)blockIdx.x * SLOTS, items = n * a.splits;
-    const int last_item = MODE == APPEND ? min(begin + SLOTS, items) - 1 : items - 1;     // whose page the CTA has to know
-    if (begin < items || (MODE != APPEND && leader)) __syncthreads();
-    for (int i0 = begin; i0 < items; i0 += stride) {
-        const int item = i0 + tid / CH, j = tid % CH;
-        const int t = item / a.splits, part = item - t * a.splits;
-        const bool in = item < items;
-        const int2 col = chunk_columns(a.r, j);
-        uint4 x[2 * kHeads][2];
-        if (in) {
-            const int from = MODE == COMMIT ? s_src[t] : t;
-            const size_t tok = (size_t)b * a.M + from;
+    const int32_t* table = a.table + (size_t)b * a.max_pages;
+    const int places = n * a.Hkv;
+    const int run = MODE == COMMIT ? ((places + (int)gridDim.x - 1) / (int)gridDim.x + SLOTS - 1) / SLOTS * SLOTS : SLOTS * a.batches;
+    const int begin = (int)blockIdx.x * run, end = min(begin + run, places);
+    const int row0 = begin / a.Hkv, row1 = (end - 1) / a.Hkv;
+    const int j = tid % CH, slot = tid / CH;
+    const int2 col = chunk_columns(a.r, j);
+    const bool turned = MODE != COMMIT && j < a.r.chunks;
+    for (int at0 = begin; at0 < end; at0 += SLOTS * kBatch) {
+        uint4 x[kBatch][4];
+        int t[kBatch], h[kBatch];
 #pragma unroll
-            for (int i = 0; i < 2 * kHeads; ++i) {
-                const int h = part + (i >> 1) * a.splits;
-                if (h < a.Hkv) {
-                    const uint16_t* src = (i & 1 ? a.v + tok * a.v_stride : a.k + tok * a.k_stride) + h * D;
-                    x[i][0] = *reinterpret_cast<const uint4*>(src + col.x);
-                    x[i][1] = *reinterpret_cast<const uint4*>(src + col.y);
-                }
-            }
+        for (int i = 0; i < kBatch; ++i) {
+            const int at = min(at0 + i * SLOTS + slot, end - 1);        // (the last place again, for those behind it)
+            t[i] = at / a.Hkv;
+            h[i] = at - t[i] * a.Hkv;
+            const size_t tok = (size_t)b * a.M + (MODE == COMMIT ? s_src[t[i]] : t[i]);
+            const uint16_t *k = a.k + tok * a.k_stride + h[i] * D, *v = a.v + tok * a.v_stride + h[i] * D;
+            x[i][0] = *reinterpret_cast<const uint4*>(k + col.x);
+            x[i][1] = *reinterpret_cast<const uint4*>(k + col.y);
+            x[i][2] = *reinterpret_cast<const uint4*>(v + col.x);
+            x[i][3] = *reinterpret_cast<const uint4*>(v + col.y);
         }
-        if (i0 == begin) {
-            const int end = ((L + last_item / a.splits) >> a.page_log2) + 1;
-            const int bad = first_bad_page(row, first_entry, end, a.num_pages, tid, kThreads);
-            if (bad < end) atomicMin(&s_bad, bad);
+        if (at0 == begin) {
+            // (a cluster's CTAs all look as far as the last row: CTA 0 needs to know what was written)
+            const int entries = ((L + (MODE == APPEND ? row1 : n - 1)) >> a.page_log2) + 1;
+            const int bad = first_bad_page(table, L >> a.page_log2, entries, a.num_pages, tid, kThreads);
+            if (bad < entries) atomicMin(&s_bad, bad);
+            for (int i = tid; i <= row1 - row0; i += kThreads) s_page[i] = table[(L + row0 + i) >> a.page_log2];
+            if (MODE != COMMIT)
+                form_angles(a.r, s_angles, row1 - row0 + 1, a.B, a.M, [&](int m, int& seq, int& t, int& place) {
+                    seq = b;
+                    t = row0 + m;
+                    place = L + t;
+                });
             __syncthreads();
         }
-        const int place = L + t, entry = place >> a.page_log2;
-        float2 cs[8];
-        const bool turned = MODE != COMMIT && j < a.r.chunks;
-        if (MODE != COMMIT && in && turned) chunk_angles(a.r, j, token_pos(a.r, b, t, a.B, a.M, place), cs);
-        if (!in || entry >= s_bad) continue;
-        const size_t dst_row = (size_t)row[entry] * page + (place & (page - 1));
-        if (!GSD_IN_BOUNDS(place < a.Lmax && dst_row < (size_t)a.num_pages * page, a.status)) continue;
 #pragma unroll
-        for (int i = 0; i < 2 * kHeads; ++i) {
-            const int h = part + (i >> 1) * a.splits;
-            if (h < a.Hkv) {
-                if (!(i & 1) && turned) turn_chunk(a.r.neighbours != 0, cs, x[i][0], x[i][1]);
-                uint16_t* dst = (i & 1 ? a.v_pages : a.k_pages) + (dst_row * a.Hkv + h) * D;
-                *reinterpret_cast<uint4*>(dst + col.x) = x[i][0];
-                *reinterpret_cast<uint4*>(dst + col.y) = x[i][1];
-            }
+        for (int i = 0; i < kBatch; ++i) {
+            const int place = L + t[i];
+            if (at0 + i * SLOTS + slot >= end || (place >> a.page_log2) >= s_bad) continue;
+            if (turned) turn_chunk<D>(a.r.neighbours != 0, s_angles[t[i] - row0], j, x[i][0], x[i][1]);
+            const size_t row = ((size_t)s_page[t[i] - row0] << a.page_log2) + (place & ((1 << a.page_log2) - 1));
+            if (!GSD_IN_BOUNDS(place < a.Lmax && row < (size_t)a.num_pages << a.page_log2, a.status)) continue;
+            uint16_t *k = a.k_pages + (row * a.Hkv + h[i]) * D, *v = a.v_pages + (row * a.Hkv + h[i]) * D;
+            *reinterpret_cast<uint4*>(k + col.x) = x[i][0];
+            *reinterpret_cast<uint4*>(k + col.y) = x[i][1];
+            *reinterpret_cast<uint4*>(v + col.x) = x[i][2];
+            *reinterpret_cast<uint4*>(v + col.y) = x[i][3];
         }
     }
-    if (begin < items && s_bad != 0x7FFFFFFF) flags |= GSD_DEV_BAD_PAGE;
+    if (begin < end && s_bad != 0x7FFFFFFF) flags |= GSD_DEV_BAD_PAGE;
     if (flags && a.status) atomicOr((unsigned*)a.status, flags);
     if (MODE != APPEND) {
         asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-        if (leader && tid == 0) {
+        if (blockIdx.x == 0 && tid == 0) {
             const int bad = s_bad;
             a.seq_lens[b] = bad == 0x7FFFFFFF ? L + n : max(L, min(L + n, bad << a.page_log2));
         }
@@ -157,14 +163,18 @@ __global__ void __launch_bounds__(kThreads) paged_advance_kernel(WriteArgs a) {
 
 constexpr int kCluster = 8;         // CTAs of a sequence that meet
 
-template <int D, int kHeads>
+template <int D>
 int launch_write(WriteArgs& a, cudaStream_t stream) {
-    a.splits = (a.Hkv + kHeads - 1) / kHeads;
+    DeviceInfo di;
+    if (device_info(&di) != 0) return GSD_ERR_CUDA;
     const int slots = kThreads / (D / 16);
-    const long long items = (long long)(a.nodes ? (a.Tcap < a.M ? a.Tcap : a.M) : a.M) * a.splits;
-    const long long ctas = (items + slots - 1) / slots;
+    const long long places = (long long)(a.nodes ? (a.Tcap < a.M ? a.Tcap : a.M) : a.M) * a.Hkv;
+    a.batches = a.nodes ? 1 : rotary_batches(places * a.B, a.Hkv, D, di.sm_count);
+    const long long ctas = (places + slots * a.batches - 1) / (slots * a.batches);
     if (!a.nodes && ctas > kCluster) {
-        GSD_CUDA_TRY(launch_dependent(paged_write_kernel<D, kHeads, APPEND>, dim3((unsigned)ctas, a.B), dim3(kThreads), 0, stream, a));
+        const dim3 grid((unsigned)ctas, a.B);
+        if (a.batches == 1) GSD_CUDA_TRY(launch_dependent(paged_write_kernel<D, 1, APPEND>, grid, dim3(kThreads), 0, stream, a));
+        else GSD_CUDA_TRY(launch_dependent(paged_write_kernel<D, 2, APPEND>, grid, dim3(kThreads), 0, stream, a));
         GSD_CUDA_TRY(launch_dependent(paged_advance_kernel, dim3((a.B + kThreads / 32 - 1) / (kThreads / 32)), dim3(kThreads), 0, stream, a));
         return GSD_OK;
     }
@@ -180,7 +190,7 @@ int launch_write(WriteArgs& a, cudaStream_t stream) {
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    GSD_CUDA_TRY(cudaLaunchKernelEx(&cfg, a.nodes ? paged_write_kernel<D, kHeads, COMMIT> : paged_write_kernel<D, kHeads, APPEND_CLUSTER>, a));
+    GSD_CUDA_TRY(cudaLaunchKernelEx(&cfg, a.nodes ? paged_write_kernel<D, 2, COMMIT> : paged_write_kernel<D, 2, APPEND_CLUSTER>, a));
     return GSD_OK;
 }
 
@@ -188,7 +198,7 @@ int write_rows(WriteArgs& a, const gsd_page_params* c, int D, cudaStream_t strea
     a.page_log2 = page_rows_log2(c, a.Lmax);
     a.max_pages = c->max_pages;
     a.num_pages = c->num_pages;
-    return D == 128 ? launch_write<128, 4>(a, stream) : launch_write<64, 4>(a, stream);
+    return D == 128 ? launch_write<128>(a, stream) : launch_write<64>(a, stream);
 }
 
 int misaligned(std::initializer_list<const void*> ptrs, unsigned bytes) {

@@ -2,7 +2,8 @@
 //
 // Of the D columns of a head the first 2 * pairs are rotated, pair i by angle_i = position[axis[i]] * freqs[i].  The work is cut
 // into chunks of 16 columns, 8 pairs: two 16-byte pieces of a head that one thread holds, so that a pair is read, turned and written
-// in one place and a rotation in place is safe.  The thread's 8 sines and cosines serve all heads it takes.
+// in one place and a rotation in place is safe.  A CTA has a run of (token, head) places; it forms the sines and cosines of its
+// tokens once, in shared memory, for all heads.
 //
 // The angle is formed in turns and reduced in 64 bits: pos * freq / 2 pi, less the nearest whole number.  In 32 bits a
 // position of 10^6 would leave an angle 2^-4 off.  What is left, at most half a turn, goes to sincospif (2 ulp).
@@ -37,6 +38,20 @@ inline bool rotation_of(const gsd_rotation* r, int D, Rotation* out) {
     return true;
 }
 
+constexpr int kRotaryThreads = 256, kRotaryBlocks = 4;
+
+// Places (token, head) of a CTA: kRotaryThreads / (D / 16) at a time, `batches` times.  More of them share their tokens' angles, as
+// long as every SM has four CTAs; and a CTA has at most rotary_tokens(D) tokens.  A thread has two of them on their way, four CTAs an
+// SM (us; 8 x 256 nodes of 64 + 8 heads and 8 x 3000 nodes of 16 + 4 heads of 64: so 12.6 and 7.8; four on their way and
+// eight batches, three CTAs an SM, 15.5 and 9.7; one and two, six CTAs 15.6 and 9.1; two and four, six CTAs, spilling, 16.0 and 11.8).
+__host__ __device__ constexpr int rotary_tokens(int D) { return kRotaryThreads / (D / 16) + 2; }
+inline int rotary_batches(long long places, int heads, int D, int sm_count) {
+    const int slots = kRotaryThreads / (D / 16);
+    int n = 1;
+    while (n < 4 && places > 4ll * sm_count * slots * n && 2 * n * slots / heads + 2 <= rotary_tokens(D)) n *= 2;
+    return n;
+}
+
 #ifdef __CUDACC__
 // The two 16-byte pieces of chunk j of a head, as element offsets.
 __device__ __forceinline__ int2 chunk_columns(const Rotation& r, int j) {
@@ -44,34 +59,33 @@ __device__ __forceinline__ int2 chunk_columns(const Rotation& r, int j) {
     return make_int2(16 * j, 16 * j + 8);
 }
 
-// The positions of a token on every axis.
-struct TokenPos {
-    long long at[GSD_ROTARY_MAX_AXES];
+// Sines and cosines of a token: [quarter of a chunk][chunk] of (cos, sin) of two pairs, so that the threads of a token's chunks
+// read without conflicts.
+template <int D>
+struct AngleTable {
+    float4 at[4][D / 16];
+    __device__ __forceinline__ float2& pair(int i) { return reinterpret_cast<float2*>(&at[(i & 7) >> 1][i >> 3])[i & 1]; }
 };
-__device__ __forceinline__ TokenPos token_pos(const Rotation& r, int b, int t, int B, int T, int place) {
-    TokenPos p;
-    const long long off = r.offsets ? r.offsets[b] : 0;
-#pragma unroll
-    for (int a = 0; a < GSD_ROTARY_MAX_AXES; ++a) {
-        if (a == 0 || a < r.axes) p.at[a] = (r.positions ? r.positions[((size_t)a * B + b) * T + t] : place) + off;
-        else p.at[a] = 0;
-    }
-    return p;
-}
 
-// (cos, sin) of the 8 pairs of chunk j.
-__device__ __forceinline__ void chunk_angles(const Rotation& r, int j, const TokenPos& pos, float2 (&cs)[8]) {
-    const uint32_t bits = r.axis_bits[j >> 1] >> (16 * (j & 1));
-    const float4 f0 = make_float4(r.freqs[8 * j], r.freqs[8 * j + 1], r.freqs[8 * j + 2], r.freqs[8 * j + 3]);
-    const float4 f1 = make_float4(r.freqs[8 * j + 4], r.freqs[8 * j + 5], r.freqs[8 * j + 6], r.freqs[8 * j + 7]);
-    const float f[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int a = (bits >> (2 * i)) & 3;
-        const long long at = a == 0 ? pos.at[0] : a == 1 ? pos.at[1] : a == 2 ? pos.at[2] : pos.at[3];
-        double turns = (double)at * ((double)f[i] * 0.15915494309189533577);     // 1 / (2 pi)
+// The angles of `n` tokens, by the whole CTA: token(m, b, t, place) says which the m-th is; its position is `place` where there are
+// no positions.  A thread has one pair of every few tokens.
+template <int D, class Token>
+__device__ __forceinline__ void form_angles(const Rotation& r, AngleTable<D>* angles, int n, int B, int T, Token token) {
+    constexpr int PAIRS = D / 2, STEP = kRotaryThreads / PAIRS;
+    const int i = threadIdx.x % PAIRS;
+    if (i >= r.chunks * 8) return;
+    const int32_t* positions = r.positions + (r.positions ? (size_t)((r.axis_bits[i >> 4] >> (2 * (i & 15))) & 3) * B * T : 0);
+    const double turns_per = (double)r.freqs[i] * 0.15915494309189533577;          // 1 / (2 pi)
+#pragma unroll 4
+    for (int m = threadIdx.x / PAIRS; m < n; m += STEP) {
+        int b, t, place;
+        token(m, b, t, place);
+        const long long pos = (long long)(r.positions ? positions[(size_t)b * T + t] : place) + (r.offsets ? r.offsets[b] : 0);
+        double turns = (double)pos * turns_per;
         turns -= rint(turns);
-        sincospif((float)(2.0 * turns), &cs[i].y, &cs[i].x);
+        float2 cs;
+        sincospif((float)(2.0 * turns), &cs.y, &cs.x);
+        angles[m].pair(i) = cs;
     }
 }
 
@@ -83,30 +97,28 @@ __device__ __forceinline__ uint32_t rotary_pack(float lo, float hi) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// The two pieces of a rotated chunk, turned.
-__device__ __forceinline__ void turn_chunk(bool neighbours, const float2 (&cs)[8], uint4& a, uint4& b) {
-    uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+// The two pieces of a rotated chunk j, turned.
+template <int D>
+__device__ __forceinline__ void turn_chunk(bool neighbours, const AngleTable<D>& angles, int j, uint4& a, uint4& b) {
+    const float4 c0 = angles.at[0][j], c1 = angles.at[1][j], c2 = angles.at[2][j], c3 = angles.at[3][j];
     if (neighbours) {
-        auto turn = [](uint32_t w, const float2& c) {
+        auto turn = [](uint32_t w, float c, float s) {
             const float u = bf16_lo(w), v = bf16_hi(w);
-            return rotary_pack(u * c.x - v * c.y, u * c.y + v * c.x);
+            return rotary_pack(u * c - v * s, u * s + v * c);
         };
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = turn(x[i], cs[i]);
-            y[i] = turn(y[i], cs[4 + i]);
-        }
+        a = make_uint4(turn(a.x, c0.x, c0.y), turn(a.y, c0.z, c0.w), turn(a.z, c1.x, c1.y), turn(a.w, c1.z, c1.w));
+        b = make_uint4(turn(b.x, c2.x, c2.y), turn(b.y, c2.z, c2.w), turn(b.z, c3.x, c3.y), turn(b.w, c3.z, c3.w));
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 c0 = cs[2 * i], c1 = cs[2 * i + 1];
-            const float u0 = bf16_lo(x[i]), u1 = bf16_hi(x[i]), v0 = bf16_lo(y[i]), v1 = bf16_hi(y[i]);
-            x[i] = rotary_pack(u0 * c0.x - v0 * c0.y, u1 * c1.x - v1 * c1.y);
-            y[i] = rotary_pack(u0 * c0.y + v0 * c0.x, u1 * c1.y + v1 * c1.x);
-        }
+        auto turn = [](uint32_t& x, uint32_t& y, const float4& c) {
+            const float u0 = bf16_lo(x), u1 = bf16_hi(x), v0 = bf16_lo(y), v1 = bf16_hi(y);
+            x = rotary_pack(u0 * c.x - v0 * c.y, u1 * c.z - v1 * c.w);
+            y = rotary_pack(u0 * c.y + v0 * c.x, u1 * c.w + v1 * c.z);
+        };
+        turn(a.x, b.x, c0);
+        turn(a.y, b.y, c1);
+        turn(a.z, b.z, c2);
+        turn(a.w, b.w, c3);
     }
-    a = make_uint4(x[0], x[1], x[2], x[3]);
-    b = make_uint4(y[0], y[1], y[2], y[3]);
 }
 #endif
 
