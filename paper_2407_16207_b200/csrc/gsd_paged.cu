@@ -41,11 +41,12 @@ __global__ void __launch_bounds__(kThreads, kRotaryBlocks) paged_write_kernel(co
     __shared__ int s_src[MODE == COMMIT ? GSD_MAX_NODES : 1];     // source row of each new place
     __shared__ int s_tot[kThreads / 32];
     __shared__ int s_bad;                                         // first table entry that names no page
-    let_successor_start();
+    if (MODE != APPEND) let_successor_start();
     const int b = blockIdx.y, tid = threadIdx.x;
     if (tid == 0) s_bad = 0x7FFFFFFF;
     __syncthreads();
     wait_for_predecessor();
+    if (MODE == APPEND) let_successor_start();      // (paged_advance_kernel, which reads the call's inputs before it waits)
     unsigned flags = 0;
     int L = a.seq_lens[b];
     if (L < 0 || L > a.Lmax) {
@@ -144,21 +145,25 @@ __global__ void __launch_bounds__(kThreads, kRotaryBlocks) paged_write_kernel(co
     }
 }
 
-// The lengths behind an append whose CTAs are too many to meet: a warp per sequence.
+// The lengths behind an append whose CTAs are too many to meet: a warp per sequence.  It starts when every CTA of the append has
+// passed its own wait - all that precedes the call is over then - works the new length out, and stores it once the append,
+// whose CTAs read the old one, is over.
 __global__ void __launch_bounds__(kThreads) paged_advance_kernel(WriteArgs a) {
     let_successor_start();
     const int b = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    wait_for_predecessor();
-    if (b >= a.B) return;
-    const int L = min(max(a.seq_lens[b], 0), a.Lmax);
-    const int n = min(min(max(a.count[b], 0), a.M), a.Lmax - L);
-    if (n == 0) {
-        if (lane == 0) a.seq_lens[b] = L;
-        return;
+    int moved = 0;
+    if (b < a.B) {
+        const int L = min(max(a.seq_lens[b], 0), a.Lmax);
+        const int n = min(min(max(a.count[b], 0), a.M), a.Lmax - L);
+        moved = L + n;
+        if (n > 0) {
+            const int first = L >> a.page_log2, end = ((L + n - 1) >> a.page_log2) + 1;
+            const int bad = __reduce_min_sync(0xFFFFFFFFu, first_bad_page(a.table + (size_t)b * a.max_pages, first, end, a.num_pages, lane, 32));
+            if (bad != end) moved = max(L, bad << a.page_log2);
+        }
     }
-    const int first = L >> a.page_log2, end = ((L + n - 1) >> a.page_log2) + 1;
-    const int bad = __reduce_min_sync(0xFFFFFFFFu, first_bad_page(a.table + (size_t)b * a.max_pages, first, end, a.num_pages, lane, 32));
-    if (lane == 0) a.seq_lens[b] = bad == end ? L + n : max(L, bad << a.page_log2);
+    wait_for_predecessor();
+    if (b < a.B && lane == 0) a.seq_lens[b] = moved;
 }
 
 constexpr int kCluster = 8;         // CTAs of a sequence that meet
