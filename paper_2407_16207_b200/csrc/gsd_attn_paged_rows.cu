@@ -109,6 +109,17 @@ __device__ __forceinline__ int visible_len(const RowsParams& p, int b) {
     return L < 0 ? 0 : (L > p.Lmax ? p.Lmax : L);
 }
 
+// n / d for n >= 0, d >= 1 and a quotient below 2^16, `inv` = 1 / d to a few ulp: the estimate is off by less than one.  A third of an
+// integer division, of which the plan takes a chain.
+__device__ __forceinline__ int div_by(int n, int d, float inv) {
+    int q = (int)((float)n * inv);
+    const int r = n - q * d;
+    if (r < 0) --q;
+    if (r >= d) ++q;
+    return q;
+}
+__device__ __forceinline__ int div_by(int n, int d) { return div_by(n, d, __fdividef(1.f, (float)d)); }
+
 // Plan by length, made by every warp for itself, a lane per sequence: the cut of each sequence's items into ranges of at most T
 // rounds (a tile for each warp); unit w is this CTA's, if there are that many.  `leave`: the merge pass's tables are written.
 template <int kRound>
@@ -121,12 +132,13 @@ __device__ __forceinline__ bool unit_by_length(const RowsParams& p, int w, int l
     const int total = __reduce_add_sync(all, t), longest = __reduce_max_sync(all, t);
     // lane k tries the k-th candidate for T, from the lower bound on (two rounds, 64 parts an item); the longest sequence
     // whole always fits, as there are no more items than CTAs
-    const int bound = max(max((total * per_seq + resident - 1) / resident, (longest + 63) / 64), 2);
+    const int bound = max(max((int)((float)total * __fdividef((float)per_seq, (float)resident)) + 1, (longest + 63) / 64), 2);
     const int T = bound + lane * max(1, bound / 16);
+    const float inv = __fdividef(1.f, (float)T);
     int units = 0;
-    for (int j = 0; j < p.B; ++j) units += (__shfl_sync(all, t, j) + T - 1) / T;
+    for (int j = 0; j < p.B; ++j) units += div_by(__shfl_sync(all, t, j) + T - 1, T, inv);
     const int best = min(longest, (int)__reduce_min_sync(all, units * per_seq <= resident ? T : 0x7FFFFFFF));
-    const int n = in ? (t + best - 1) / best : 0;
+    const int n = in ? div_by(t + best - 1, best) : 0;
     int end = n;                                            // ranges up to and with this sequence, per item
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -141,10 +153,10 @@ __device__ __forceinline__ bool unit_by_length(const RowsParams& p, int w, int l
     u.L = __shfl_sync(all, L, u.b);
     u.nsplit = __shfl_sync(all, n, u.b);
     const int r = w - __shfl_sync(all, end - n, u.b) * per_seq;
-    u.split = r / per_seq;
+    u.split = div_by(max(r, 0), per_seq);
     const int item = r - u.split * per_seq;
-    u.c = item / p.plan.tiles_per_unit;
-    u.row0 = item % p.plan.tiles_per_unit;
+    u.c = div_by(max(item, 0), p.plan.tiles_per_unit);
+    u.row0 = item - u.c * p.plan.tiles_per_unit;
     u.slot = w;
     return w < __shfl_sync(all, end, 31) * per_seq;
 }
@@ -164,6 +176,12 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     Unit u;
     if (p.plan.balanced == 3) {
         wait_for_predecessor();
+        // the table's lines, a part a CTA, while the lengths come: its look-ups are the next trip
+        const int lines = (p.Lmax >> p.pages.page_log2) / 32 + 1;            // of a row, 128 bytes each
+        for (int i = blockIdx.x * T::THREADS + tid; i < p.B * lines; i += gridDim.x * T::THREADS) {
+            const int row = i / lines, at = (i - row * lines) * 32;
+            if (at < p.pages.max_pages) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.pages.table + (size_t)row * p.pages.max_pages + at) : "memory");
+        }
         if (!unit_by_length<WARPS>(p, blockIdx.x, lane, blockIdx.x == 0 && warp == 0, u)) return;
     } else {
         int item;
@@ -222,6 +240,21 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
             cp_async16(stage + T::TILE + off, r < rows ? v + step : p.v_pages, bytes);
         }
     };
+    // The query rows, asked for before the keys fill the queues (behind 128 KB of them an SM they took 2.5 us): a warp for every
+    // eight rows.
+    static_assert(NT <= WARPS, "a row group a warp");
+    uint32_t qw[KS][2];
+    if (warp < NT) {
+        const int row = row0 + warp * 8 + i8;
+        const bool in = row < R;
+        const int rr = in ? row : 0;
+        const __nv_bfloat16* q = p.q + (((size_t)b * N + rr / G) * p.Hq + c * G + rr % G) * D + 2 * j4;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qw[ks][0] = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16) : 0u;
+            qw[ks][1] = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16 + 8) : 0u;
+        }
+    }
     int pages = find_pages(0), pages_next = find_pages(32);
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) {
@@ -229,20 +262,16 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         cp_async_commit();
     }
 
-    // ---- the query rows as fragments (rows are columns of the products): a warp for every eight rows puts them where all
-    // warps find them
+    // the mask words of the draft tiles, which come last, as a trip of their own
+    for (int t = max(first, nPT); t < t_end; t += WARPS)
+        for (int node = row0 / G + lane; node <= min(row0 + T::ROWS - 1, R - 1) / G; node += 32)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.mask + ((size_t)b * N + node) * p.W + ((t - nPT) * kKeys >> 5)) : "memory");
+    // ---- the query rows as fragments (rows are columns of the products), where all warps find them
     const uint32_t q_at = smem_u32(smem) + T::Q_AT + lane * 8;
+    if (warp < NT) {
 #pragma unroll
-    for (int nt = warp; nt < NT; nt += WARPS) {
-        const int row = row0 + nt * 8 + i8;
-        const bool in = row < R;
-        const int rr = in ? row : 0;
-        const __nv_bfloat16* q = p.q + (((size_t)b * N + rr / G) * p.Hq + c * G + rr % G) * D + 2 * j4;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const uint32_t lo = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16) : 0u, hi = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16 + 8) : 0u;
-            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(q_at + (nt * KS + ks) * 256), "r"(lo), "r"(hi) : "memory");
-        }
+        for (int ks = 0; ks < KS; ++ks)
+            asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(q_at + (warp * KS + ks) * 256), "r"(qw[ks][0]), "r"(qw[ks][1]) : "memory");
     }
     __syncthreads();
     uint2 qf[NT == 1 ? KS : 1];
@@ -405,7 +434,7 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     }
     __syncthreads();
     // a thread takes four columns of a row
-#pragma unroll 1
+#pragma unroll 2
     for (int x = tid; x < NT * 8 * (D / 4); x += T::THREADS) {
         const int r8 = x & 7, quad = (x >> 3) % (D / 4), nt = (x >> 3) / (D / 4);
         const int row = row0 + nt * 8 + r8;
