@@ -3,16 +3,17 @@
 //
 //   s_j = scale <q, K_j>,   p_j = 2^(s_j log2(e) - m),   out = sum_j p_j V_j / sum_j p_j
 //
-// A tile is 16 keys: a page holds whole tiles, so each lies in one place.  Every warp has tiles of its own, a ring of them in
-// shared memory filled by asynchronous copies, and nothing to wait for but its own; the warps meet once, at the end.  Lane l of
-// a warp looks up the page of the l-th of its next 32 tiles.  Both products are transposed, S^T = K Q^T and O^T = V^T P^T, so
-// that 8 rows fill an instruction (16 keys or 16 columns by 8 rows); the weights are turned round by a movmatrix.  A row's
-// running maximum is raised when a score exceeds it by more than 2^kLag: the weights are rounded to bf16, whose relative
-// step does not depend on their size, and sums stay fp32.
+// A tile is 16 keys: a page holds whole tiles, so each lies in one place and takes one TMA copy each of K and V.  Every warp has
+// tiles of its own, a ring of them in shared memory, and nothing to wait for but its own copies; the warps meet once, at the
+// end.  Lane l of a warp looks up the page of the l-th of its next 32 tiles.  The tile that holds the end of the sequence is
+// copied as the 16 rows up to the end (rows before the page's first come back as zeros), so that nothing behind the end is read.
+// Both products are transposed, S^T = K Q^T and O^T = V^T P^T, so that 8 rows fill an instruction (16 keys or 16 columns by 8
+// rows); the weights are turned round by a movmatrix.  A row's running maximum is raised when a score exceeds it by more than
+// 2^kLag: the weights are rounded to bf16, whose relative step does not depend on their size, and sums stay fp32.
 //
 // The work is dealt out by length inside the kernel for up to 32 sequences: every item (a group of rows of a sequence and
 // kv head) is cut into ranges of at most T rounds of keys, T the least with which all ranges are resident at once.
-#include "gsd_internal.cuh"
+#include "gsd_tma.cuh"
 #include <cuda_bf16.h>
 #include <math_constants.h>
 
@@ -23,7 +24,7 @@ constexpr int kKeys = 16;                    // keys of a warp's tile
 constexpr float kLag = 8.f;                  // log2
 
 struct RowsParams {
-    const __nv_bfloat16 *q, *k_pages, *v_pages, *draft_k, *draft_v;
+    const __nv_bfloat16* q;
     const uint32_t* mask;
     const int32_t* seq_lens;
     __nv_bfloat16* out;
@@ -37,6 +38,8 @@ struct RowsParams {
     int B, N, Hq, Hkv, Lmax, G, W, R;
     int slots;
     float scale_log2;
+    unsigned long long wait_limit_ns;
+    int withhold_first_k;    // test hook: every warp leaves out the K copy of its first tile
 };
 
 template <int D, int NT>
@@ -52,17 +55,9 @@ struct RowsGeo {
     static constexpr int VALUES = MTILES * 4 + 4;               // of a lane and 8 rows, when the warps' results are brought together
     static constexpr int MEET = WARPS * NT * VALUES * 32 * 4;
     static constexpr int Q_AT = RING > MEET ? RING : MEET;      // query fragments: [row group][k-step][lane] pairs of registers
-    static constexpr int SMEM = Q_AT + NT * (D / 16) * 32 * 8;
+    static constexpr int SMEM = Q_AT + NT * (D / 16) * 32 * 8 + 1024;       // (alignment)
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16-byte async copy; src_bytes == 0 writes zeros and reads nothing
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int src_bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
     uint2 v;
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
@@ -97,6 +92,17 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
     uint32_t d;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
+}
+
+// Bounded wait, by the whole warp; false: it gave up.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
+    bool ok = mbar_try_wait(bar, parity);
+    if (!__all_sync(0xFFFFFFFFu, ok)) {
+        const unsigned long long t0 = global_ns();
+        while (!ok && global_ns() - t0 <= limit_ns) ok = mbar_try_wait(bar, parity);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+    }
+    return ok;
 }
 
 // What a CTA works on: rows of (sequence b, kv head c), keys of one of `nsplit` ranges.
@@ -162,17 +168,30 @@ __device__ __forceinline__ bool unit_by_length(const RowsParams& p, int w, int l
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCKS) attn_paged_rows_kernel(RowsParams p) {
+__global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCKS) attn_paged_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_dk,
+                       const __grid_constant__ CUtensorMap tm_dv, const RowsParams p) {
     using T = RowsGeo<D, NT>;
     constexpr int KS = D / 16;              // k-steps of the product with K
     constexpr int MTL = T::MTILES, WARPS = T::WARPS, ST = T::STAGES;
-    constexpr int CH = D / 8, LANE_ROWS = 32 / CH;             // 16-byte pieces of a row; rows a copy of the warp takes
-    extern __shared__ __align__(128) unsigned char smem[];
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) unsigned long long s_full[WARPS * ST];
+    unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
 
     if (p.slots > 0) let_successor_start();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int i8 = lane >> 2, j4 = lane & 3;
     const int N = p.N, G = p.G, R = p.R;
+    const uint32_t full = smem_u32(s_full) + warp * (ST * 8);      // the warp's barriers, one a stage
+    if (lane == 0) {
+        for (int s = 0; s < ST; ++s) mbar_init(full + 8 * s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (warp == 0) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
+        }
+    }
+    __syncwarp();
     Unit u;
     if (p.plan.balanced == 3) {
         wait_for_predecessor();
@@ -206,9 +225,8 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     const int first = t_begin + warp;
     const int n_tiles = max(0, (t_end - first + WARPS - 1) / WARPS);
 
-    // ---- the ring: K and V tiles of 16 rows, 16-byte pieces swizzled by the row
+    // ---- the ring: K and V tiles of 16 rows, blocks of 64 columns
     const uint32_t ring = smem_u32(smem) + warp * (ST * 2 * T::TILE);
-    const size_t row_elems = (size_t)p.Hkv * D;
     const int32_t* table = p.pages.table + (size_t)b * p.pages.max_pages;
     // the pages of the warp's tiles i0 + lane; -1: none (draft tiles, no such tile, no such page)
     auto find_pages = [&](int i0) -> int {
@@ -219,26 +237,24 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         if (p.status) atomicOr((unsigned*)p.status, GSD_DEV_BAD_PAGE);
         return -1;
     };
-    const int my_row = lane / CH, my_piece = lane % CH;
-    auto issue = [&](int i, uint32_t stage, int pages) {
+    auto issue = [&](int i, int stage, int pages) {
         const int t = first + i * WARPS;
-        const bool draft = t >= nPT;
-        const int key0 = (draft ? t - nPT : t) * kKeys;
         const int page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
-        const int rows = draft ? N - key0 : page < 0 ? 0 : L - key0;         // of the tile that are read
-        const size_t row = draft ? (size_t)b * N + key0 : ((size_t)max(page, 0) << p.pages.page_log2) + (key0 & ((1 << p.pages.page_log2) - 1));
-        const size_t at = (row + my_row) * row_elems + (size_t)c * D + my_piece * 8;
-        const __nv_bfloat16* k = (draft ? p.draft_k : p.k_pages) + at;
-        const __nv_bfloat16* v = (draft ? p.draft_v : p.v_pages) + at;
-#pragma unroll
-        for (int x = 0; x < kKeys / LANE_ROWS; ++x) {
-            const int r = x * LANE_ROWS + my_row;
-            const uint32_t off = (uint32_t)(r * (D * 2) + ((my_piece ^ (r & 7)) << 4));
-            const int bytes = r < rows ? 16 : 0;
-            const size_t step = r < rows ? (size_t)(x * LANE_ROWS) * row_elems : 0;
-            cp_async16(stage + off, r < rows ? k + step : p.k_pages, bytes);
-            cp_async16(stage + T::TILE + off, r < rows ? v + step : p.v_pages, bytes);
+        if (lane == 0) {
+            const uint32_t dst = ring + stage * (2 * T::TILE), bar = full + 8 * stage;
+            mbar_expect_tx(bar, 2 * T::TILE);
+            if (t >= nPT) {
+                if (!(p.withhold_first_k && i == 0)) tma_load_4d(dst, &tm_dk, bar, 0, (t - nPT) * kKeys, c * (D / 64), b);
+                tma_load_4d(dst + T::TILE, &tm_dv, bar, 0, (t - nPT) * kKeys, c * (D / 64), b);
+            } else {
+                const int key0 = t * kKeys;
+                // (no such page: from behind the pool, zeros)
+                const int row = (key0 & ((1 << p.pages.page_log2) - 1)) + min(0, L - key0 - kKeys), at = page < 0 ? p.pages.num_pages : page;
+                if (!(p.withhold_first_k && i == 0)) tma_load_4d(dst, &tm_k, bar, 0, row, c * (D / 64), at);
+                tma_load_4d(dst + T::TILE, &tm_v, bar, 0, row, c * (D / 64), at);
+            }
         }
+        __syncwarp();
     };
     // The query rows, asked for before the keys fill the queues (behind 128 KB of them an SM they took 2.5 us): a warp for every
     // eight rows.
@@ -256,11 +272,7 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         }
     }
     int pages = find_pages(0), pages_next = find_pages(32);
-#pragma unroll
-    for (int s = 0; s < ST - 1; ++s) {
-        if (s < n_tiles) issue(s, ring + s * (2 * T::TILE), pages);
-        cp_async_commit();
-    }
+    for (int s = 0; s < min(ST, n_tiles); ++s) issue(s, s, pages);
 
     // the mask words of the draft tiles, which come last, as a trip of their own
     for (int t = max(first, nPT); t < t_end; t += WARPS)
@@ -289,25 +301,21 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         m_run[nt][0] = m_run[nt][1] = -CUDART_INF_F;
         l_run[nt][0] = l_run[nt][1] = 0.f;
     }
-    // where the lane's rows of the matrices start: K keys (lane & 15), pieces + (lane >> 4); V keys (lane & 7) + 8 (lane >> 4)
+    // where the lane's rows of the matrices start: K keys (lane & 15), pieces + (lane >> 4); V keys (lane & 7) + 8 (lane >> 4).  A
+    // piece of 16 bytes sits at its number exclusive-or'ed with the low bits of its row's (the copies' swizzle).
     const int k_row = lane & 15, v_row = (lane & 7) + ((lane >> 4) << 3);
-    uint32_t stage = ring, fill = ring + (ST - 1) * (2 * T::TILE);
-    const uint32_t ring_end = ring + ST * (2 * T::TILE);
+    const uint32_t k_at = k_row * 128 + (((lane >> 4) ^ (k_row & 7)) << 4), v_at = v_row * 128 + ((((lane >> 3) & 1) ^ (v_row & 7)) << 4);
+    auto piece_pair = [](uint32_t at, int x) -> uint32_t { return (at ^ ((x & 3) << 5)) + (x >> 2) * (kKeys * 128); };   // pieces 2 x and 2 x + 1
+    int stage = 0;
+    uint32_t parity = 0;
+    bool ok = true;
+    int done = 0;                           // tiles that have landed
 #pragma unroll 1
     for (int i = 0; i < n_tiles; ++i) {
-        const int ahead = i + ST - 1;
-        if ((ahead & 31) == 0) {
-            pages = pages_next;
-            pages_next = find_pages(ahead + 32);
-        }
-        if (ahead < n_tiles) issue(ahead, fill, pages);
-        cp_async_commit();
-        fill = stage;
-        cp_async_wait<ST - 1>();
-        __syncwarp();
-        const uint32_t sk = stage, sv = stage + T::TILE;
-        stage += 2 * T::TILE;
-        if (stage == ring_end) stage = ring;
+        ok = wait_warp(full + 8 * stage, parity, p.wait_limit_ns);
+        if (!ok) break;
+        ++done;
+        const uint32_t sk = ring + stage * (2 * T::TILE), sv = sk + T::TILE;
 
         // S^T = K Q^T: 16 keys (i8, i8 + 8) x 8 rows; two chains at least
         constexpr int CHAINS = NT == 1 ? 2 : 1;
@@ -319,7 +327,7 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             uint32_t a[4];
-            ldmatrix_x4(a, sk + k_row * (D * 2) + (((ks * 2 + (lane >> 4)) ^ (k_row & 7)) << 4));
+            ldmatrix_x4(a, sk + piece_pair(k_at, ks));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const uint2 q = NT == 1 ? qf[NT == 1 ? ks : 0] : lds64(q_at + (nt * KS + ks) * 256);
@@ -346,8 +354,8 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
                     s[nt][e + 2] = (w >> (i8 + 8)) & 1u ? s[nt][e + 2] * p.scale_log2 : -CUDART_INF_F;
                 }
         } else {
-            const int key = t * kKeys + i8;
-            const bool lo = key < L, hi = key + 8 < L;
+            const int before = t * kKeys + kKeys - L;       // keys of the last tile that the tile before it has covered, or zeros
+            const bool lo = i8 >= before, hi = i8 + 8 >= before;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -398,13 +406,27 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
 #pragma unroll
         for (int mt = 0; mt < MTL; ++mt) {
             uint32_t a[4];
-            ldmatrix_x4_trans(a, sv + v_row * (D * 2) + (((mt * 2 + ((lane >> 3) & 1)) ^ (v_row & 7)) << 4));
+            ldmatrix_x4_trans(a, sv + piece_pair(v_at, mt));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) mma_bf16(o[nt][mt], a, pf[nt][0], pf[nt][1]);
         }
         __syncwarp();                       // the stage has been read: a copy may take its place
+        const int ahead = i + ST;
+        if ((ahead & 31) == 0) {
+            pages = pages_next;
+            pages_next = find_pages(ahead + 32);
+        }
+        if (ahead < n_tiles) issue(ahead, stage, pages);
+        if (++stage == ST) {
+            stage = 0;
+            parity ^= 1;
+        }
     }
-    cp_async_wait<0>();
+    if (!ok) {
+        // gave up: the copies under way have to land before the memory is used again
+        if (lane == 0 && p.status) atomicOr((unsigned*)p.status, GSD_DEV_WAIT_EXPIRED);
+        for (int i = done; i < min(done + ST, n_tiles); ++i) wait_warp(full + 8 * (i % ST), (uint32_t)(i / ST) & 1u, p.wait_limit_ns);
+    }
 
     // ---- the warps' results meet in the memory of the rings
 #pragma unroll
@@ -471,8 +493,16 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
 template <int D, int NT>
 int launch_t(const AttnArgs& a) {
     RowsParams p;
-    p.q = (const __nv_bfloat16*)a.q; p.draft_k = (const __nv_bfloat16*)a.draft_k; p.draft_v = (const __nv_bfloat16*)a.draft_v;
-    p.k_pages = (const __nv_bfloat16*)a.k_cache; p.v_pages = (const __nv_bfloat16*)a.v_cache; p.pages = a.pages;
+    p.q = (const __nv_bfloat16*)a.q;
+    p.pages = a.pages;
+    CUtensorMap tk, tv, tdk, tdv;
+    int rc;
+    if ((rc = make_rows_map(&tk, a.k_cache, D, a.Hkv, 1 << a.pages.page_log2, a.pages.num_pages, kKeys)) != GSD_OK) return rc;
+    if ((rc = make_rows_map(&tv, a.v_cache, D, a.Hkv, 1 << a.pages.page_log2, a.pages.num_pages, kKeys)) != GSD_OK) return rc;
+    if ((rc = make_rows_map(&tdk, a.draft_k, D, a.Hkv, a.N, a.B, kKeys)) != GSD_OK) return rc;
+    if ((rc = make_rows_map(&tdv, a.draft_v, D, a.Hkv, a.N, a.B, kKeys)) != GSD_OK) return rc;
+    p.wait_limit_ns = g_wait_limit_ns;
+    p.withhold_first_k = g_withhold_first_k;
     p.mask = a.mask; p.seq_lens = a.seq_lens; p.out = (__nv_bfloat16*)a.out; p.status = a.status;
     p.B = a.B; p.N = a.N; p.Hq = a.Hq; p.Hkv = a.Hkv; p.Lmax = a.Lmax; p.G = a.G; p.W = a.W; p.R = a.N * a.G;
     p.scale_log2 = a.scale_log2; p.plan = a.plan.dev; p.slots = a.plan.slots;
@@ -490,7 +520,7 @@ int launch_t(const AttnArgs& a) {
             if (dev >= 0 && dev < 64) done[dev] = true;
         }
     }
-    GSD_CUDA_TRY(launch_dependent(attn_paged_rows_kernel<D, NT>, dim3(a.plan.ctas), dim3(RowsGeo<D, NT>::THREADS), smem, a.stream, p));
+    GSD_CUDA_TRY(launch_dependent(attn_paged_rows_kernel<D, NT>, dim3(a.plan.ctas), dim3(RowsGeo<D, NT>::THREADS), smem, a.stream, tk, tv, tdk, tdv, p));
     return GSD_OK;
 }
 

@@ -35,17 +35,12 @@
 // pages (each takes a minute to compile).
 #pragma once
 #include "gsd_internal.cuh"
-#include <cuda.h>
+#include "gsd_tma.cuh"
 #include <cuda_bf16.h>
 #include <math_constants.h>
 #include <stdio.h>
 
 namespace gsd {
-
-// Test hook (see gsd_debug_attn_wait): a shorter limit and, optionally, a CTA's first K tile
-// withheld so that a wait really runs out.
-extern unsigned long long g_wait_limit_ns;
-extern int g_withhold_first_k;
 
 namespace {
 
@@ -94,7 +89,6 @@ constexpr float kRescaleThreshold = 8.0f;
 // Units of work per CTA decoded in the prologue.  A fixed plan with more is launched in several parts;
 // only the plans from tables decode further units where they are needed.
 constexpr int kUnitTable = 128;
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // default limit of every in-kernel wait
 
 // What every bounded wait looks at, in shared memory: word 0 is raised by the first wait that
 // gives up (all other waits then return within a few polls), words 2-3 hold the time limit.
@@ -151,30 +145,6 @@ struct TcParams {
 };
 
 // ------------------------------------------------------------------ PTX wrappers
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long global_ns() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-
 // Bounded wait.  Returns false when the wait gave up (time limit, or another role raised the
 // abort flag); the caller then leaves its loop.  `ignore_abort` is for the final drain.
 __device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag,
@@ -202,13 +172,6 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                                int32_t* status) {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status));
-}
-
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar,
-                                            int c0, int c1, int c2, int c3) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 
 __device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* map, uint32_t bar,
@@ -1492,42 +1455,6 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 }
 
 // ------------------------------------------------------------------ host side
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void* ptr = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres);
-        if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !ptr) {
-            if (e != cudaSuccess) set_cuda_error(e, "cudaGetDriverEntryPoint(cuTensorMapEncodeTiled)");
-            else set_error_text("cuTensorMapEncodeTiled is not available in this driver");
-            return nullptr;
-        }
-        fn = (EncodeTiledFn)ptr;
-    }
-    return fn;
-}
-
-int encode_map(CUtensorMap* m, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return GSD_ERR_CUDA;
-    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        char msg[96];
-        snprintf(msg, sizeof msg, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
-        set_error_text(msg);
-        return GSD_ERR_CUDA;
-    }
-    return GSD_OK;
-}
-
 // [d3][d2][d1][D] bf16 tensor; box = 64 columns x box1 x box2 x 1, 128-byte swizzle, zero fill
 int make_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t d1, uint64_t d2, uint64_t d3, uint32_t box1, uint32_t box2) {
     const cuuint64_t dims[4] = {(cuuint64_t)HD, d1, d2, d3};
@@ -1536,14 +1463,6 @@ int make_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t d1, uint64_
     return encode_map(m, base, 4, dims, strides, box);
 }
 
-// [P][rows][Hkv][HD], 8 rows of a head from any row on, the column blocks one behind the other
-int make_group_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t Hkv, uint64_t rows, uint64_t P) {
-    const cuuint64_t row = HD * 2 * Hkv;
-    const cuuint64_t dims[4] = {64, rows, HD / 64 * Hkv, P};
-    const cuuint64_t strides[3] = {row, 128, rows * row};
-    const cuuint32_t box[4] = {64, 8, (cuuint32_t)(HD / 64), 1};
-    return encode_map(m, base, 4, dims, strides, box);
-}
 // Pages [P][page][Hkv][HD], a piece of one: box / 8 such groups
 int make_page_map(CUtensorMap* m, const void* base, uint64_t HD, uint64_t Hkv, uint64_t page, uint64_t P, uint32_t box) {
     const cuuint64_t row = HD * 2 * Hkv;
@@ -1567,10 +1486,10 @@ static int launch_tc(const AttnArgs& a) {
         if constexpr (HD == 128) {
             if ((rc = make_page_map(&pages.k, a.k_cache, HD, a.Hkv, page, P, box)) != GSD_OK) return rc;
             if ((rc = make_page_map(&pages.v, a.v_cache, HD, a.Hkv, page, P, box)) != GSD_OK) return rc;
-            if ((rc = make_group_map(&tk, a.k_cache, HD, a.Hkv, page, P)) != GSD_OK) return rc;
-            if ((rc = make_group_map(&tv, a.v_cache, HD, a.Hkv, page, P)) != GSD_OK) return rc;
-            if ((rc = make_group_map(&tdk, a.draft_k, HD, a.Hkv, a.N, a.B)) != GSD_OK) return rc;
-            if ((rc = make_group_map(&tdv, a.draft_v, HD, a.Hkv, a.N, a.B)) != GSD_OK) return rc;
+            if ((rc = make_rows_map(&tk, a.k_cache, HD, a.Hkv, page, P, 8)) != GSD_OK) return rc;
+            if ((rc = make_rows_map(&tv, a.v_cache, HD, a.Hkv, page, P, 8)) != GSD_OK) return rc;
+            if ((rc = make_rows_map(&tdk, a.draft_k, HD, a.Hkv, a.N, a.B, 8)) != GSD_OK) return rc;
+            if ((rc = make_rows_map(&tdv, a.draft_v, HD, a.Hkv, a.N, a.B, 8)) != GSD_OK) return rc;
         } else {
             if ((rc = make_map(&tk, a.k_cache, HD, a.Hkv, page, P, 1, box)) != GSD_OK) return rc;
             if ((rc = make_map(&tv, a.v_cache, HD, a.Hkv, page, P, 1, box)) != GSD_OK) return rc;
