@@ -404,8 +404,8 @@ AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
     const int rounds = ((p->Lmax + 15) / 16 + (p->N + 15) / 16 + 7) / 8;        // of a tile for each warp
     if (p->num_splits > 0) {
         pl.dev.splits_a = p->num_splits;
-    } else if (pl.items + p->Hkv * pl.dev.tiles_per_unit <= resident && rounds > 2 && p->B <= 32) {
-        // the kernel deals the work out by length; all items of a sequence are cut alike, so with fewer CTAs to spare than a
+    } else if (pl.items + p->Hkv * pl.dev.tiles_per_unit <= resident && rounds > 2 && p->B > 1 && p->B <= 32) {
+        // the kernel deals the work out by length (which takes it 0.7 us, and one sequence needs none of it); all items of a sequence are cut alike, so with fewer CTAs to spare than a
         // sequence has items there is nothing to cut
         pl.dev.balanced = 3;
         pl.ctas = pl.slots = resident;                  // unit w owns slot w

@@ -142,7 +142,9 @@ __device__ __forceinline__ bool unit_by_length(const RowsParams& p, int w, int l
     const int T = bound + lane * max(1, bound / 16);
     const float inv = __fdividef(1.f, (float)T);
     int units = 0;
-    for (int j = 0; j < p.B; ++j) units += div_by(__shfl_sync(all, t, j) + T - 1, T, inv);
+    for (int j0 = 0; j0 < p.B; j0 += 4)                     // (lanes behind the last sequence have no rounds)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) units += div_by(__shfl_sync(all, t, j0 + j) + T - 1, T, inv);
     const int best = min(longest, (int)__reduce_min_sync(all, units * per_seq <= resident ? T : 0x7FFFFFFF));
     const int n = in ? div_by(t + best - 1, best) : 0;
     int end = n;                                            // ranges up to and with this sequence, per item
@@ -193,14 +195,16 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     }
     __syncwarp();
     Unit u;
-    if (p.plan.balanced == 3) {
-        wait_for_predecessor();
+    wait_for_predecessor();
+    {
         // the table's lines, a part a CTA, while the lengths come: its look-ups are the next trip
         const int lines = (p.Lmax >> p.pages.page_log2) / 32 + 1;            // of a row, 128 bytes each
         for (int i = blockIdx.x * T::THREADS + tid; i < p.B * lines; i += gridDim.x * T::THREADS) {
             const int row = i / lines, at = (i - row * lines) * 32;
             if (at < p.pages.max_pages) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.pages.table + (size_t)row * p.pages.max_pages + at) : "memory");
         }
+    }
+    if (p.plan.balanced == 3) {
         if (!unit_by_length<WARPS>(p, blockIdx.x, lane, blockIdx.x == 0 && warp == 0, u)) return;
     } else {
         int item;
@@ -209,7 +213,6 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         u.row0 = item % p.plan.tiles_per_unit;
         u.b = pair / p.Hkv;
         u.c = pair % p.Hkv;
-        wait_for_predecessor();
         u.L = visible_len(p, u.b);
     }
     u.row0 *= T::ROWS;
