@@ -378,14 +378,23 @@ int attn_paged_params_ok(const gsd_attn_params* p, const gsd_page_params* c) {
     }
     return page_rows_log2(c, p->Lmax) < 0 ? GSD_ERR_BAD_SHAPE : GSD_OK;
 }
-// The kernel for few rows reads the cache once for 32 rows (64 at D = 64); the tcgen05 kernel for up to 256.
-int attn_paged_pick_kernel(const gsd_attn_params* p) {
+// The kernel for few rows reads the cache once for up to 32 rows (48 at D = 64), the tcgen05 kernel for up to 256.  us, few rows and
+// tcgen05; D 128: 1 x 32 heads, L 2048, R = 24 13.9 and 15.8, 32 15.0 and 15.9, 48 15.9 and 16.0, 64 17.9 and 16.1; L 200, R = 48 8.6
+// and 11.5; L 8192, R = 32 30.7 and 32.8, 48 36.4 and 32.9; 8 x 64/8, L 2048-4096, R = 32 28.2 and 29.1, 40 34.6 and 29.9; with more
+// pairs than SMs, 32 x 64/8, L 500-2500, R = 24 44.2 and 45.3, 32 49.2 and 46.7; 8 x 32, L 500-1500, R = 32 36.5 and 33.7.  D 64: 4 x
+// 32/8, L 1000-2000, R = 48 15.1 and 15.9, 64 17.1 and 16.0, L 150-300, R = 32 10.0 and 11.0, 48 12.4 and 11.0; 16 x 32/8, L
+// 1000-2000, R = 32 21.1 and 28.1, 48 26.2 and 28.4, 64 31.2 and 28.5.
+int attn_paged_pick_kernel(const gsd_attn_params* p, int sm_count) {
     if (p->kernel != GSD_ATTN_AUTO) return p->kernel;
-    const int G = p->Hq / p->Hkv, R = p->N * G;
-    return attn_tcgen05_supports(p->D, G) && R > (p->D == 64 ? 64 : 32) ? GSD_ATTN_TCGEN05 : GSD_ATTN_MMA;
+    const int G = p->Hq / p->Hkv, R = p->N * G, pairs = p->B * p->Hkv;
+    if (!attn_tcgen05_supports(p->D, G)) return GSD_ATTN_MMA;
+    bool few;
+    if (p->D == 64) few = R <= 32 || (R <= 48 && p->Lmax >= 512);
+    else few = R <= 24 || (R <= 32 && pairs <= sm_count) || (R <= 48 && 2 * pairs <= sm_count && p->Lmax <= 2048);
+    return few ? GSD_ATTN_MMA : GSD_ATTN_TCGEN05;
 }
 AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
-    if (attn_paged_pick_kernel(p) == GSD_ATTN_TCGEN05) {
+    if (attn_paged_pick_kernel(p, sm_count) == GSD_ATTN_TCGEN05) {
         gsd_attn_params as = *p;
         as.kernel = GSD_ATTN_TCGEN05;
         as.num_splits = std::max(p->num_splits, 0);

@@ -529,10 +529,10 @@ int launch_t(const AttnArgs& a) {
 
 }  // namespace
 
-// Stacked rows of an item: as few items as 32 rows each (64 at D = 64, whose accumulators are half as wide) allow, with the row
+// Stacked rows of an item: as few items as 32 rows each (48 at D = 64, whose accumulators are half as wide) allow, with the row
 // groups shared out evenly.
 int attn_paged_rows(int R, int D) {
-    const int most = D == 64 ? 64 : 32, items = (R + most - 1) / most, groups = (R + 7) / 8;
+    const int most = D == 64 ? 48 : 32, items = (R + most - 1) / most, groups = (R + 7) / 8;
     const int even = (groups + items - 1) / items;
     return 8 * (even > 4 ? (even + 1) / 2 * 2 : even);
 }
@@ -549,7 +549,6 @@ int launch_attn_paged_rows(const AttnArgs& a) {
         case 24064: return launch_t<64, 3>(a);
         case 32064: return launch_t<64, 4>(a);
         case 48064: return launch_t<64, 6>(a);
-        case 64064: return launch_t<64, 8>(a);
     }
     return GSD_ERR_BAD_SHAPE;
 }
