@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kKeys = 16;                    // keys of a warp's tile
 constexpr float kLag = 8.f;                  // log2
+constexpr int kTableLines = 16;              // lines of the page table that a CTA asks for ahead of time
 
 struct RowsParams {
     const __nv_bfloat16* q;
@@ -196,13 +197,12 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     __syncwarp();
     Unit u;
     wait_for_predecessor();
-    {
-        // the table's lines, a part a CTA, while the lengths come: its look-ups are the next trip
-        const int lines = (p.Lmax >> p.pages.page_log2) / 32 + 1;            // of a row, 128 bytes each
-        for (int i = blockIdx.x * T::THREADS + tid; i < p.B * lines; i += gridDim.x * T::THREADS) {
-            const int row = i / lines, at = (i - row * lines) * 32;
-            if (at < p.pages.max_pages) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.pages.table + (size_t)row * p.pages.max_pages + at) : "memory");
-        }
+    if (tid < kTableLines) {
+        // the table's first lines, a few a CTA, while the lengths come: its look-ups are the next trip
+        const int lines = (p.Lmax >> p.pages.page_log2) / 32 + 1, i = blockIdx.x * kTableLines + tid;      // of a row, 128 bytes each
+        const int row = i / lines, at = (i - row * lines) * 32;
+        if (row < p.B && at < p.pages.max_pages)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.pages.table + (size_t)row * p.pages.max_pages + at) : "memory");
     }
     if (p.plan.balanced == 3) {
         if (!unit_by_length<WARPS>(p, blockIdx.x, lane, blockIdx.x == 0 && warp == 0, u)) return;

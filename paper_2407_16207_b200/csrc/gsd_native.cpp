@@ -707,7 +707,8 @@ PyObject* py_append_kv_paged(PyObject*, PyObject* const* argv, Py_ssize_t nargs)
 // (q, k, freqs, positions, offsets, axes, pairs, out)
 PyObject* py_rotary(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
     GSD_PY_BEGIN(8)
-    if (argv[7] != Py_None || argv[3] == Py_None) Py_RETURN_NONE;
+    PyObject* out = argv[7];
+    if ((out != Py_None && (!PyTuple_CheckExact(out) || PyTuple_GET_SIZE(out) != 2)) || argv[3] == Py_None) Py_RETURN_NONE;
     gsd_rotary_params p = {};
     const at::Tensor* q = rows_arg(a, 0, &p.q_stride);
     const at::Tensor* k = argv[1] == Py_None ? nullptr : rows_arg(a, 1, &p.k_stride);
@@ -718,14 +719,27 @@ PyObject* py_rotary(PyObject*, PyObject* const* argv, Py_ssize_t nargs) {
     if (k && !k->sizes().equals({p.B, p.T, p.Hkv, p.D})) Py_RETURN_NONE;
     Turn turn{};
     if (!turn_args(a, 2, p.B, p.T, turn)) Py_RETURN_NONE;
+    at::Tensor qo, ko;
+    if (out != Py_None) {
+        PyObject* const given[2] = {PyTuple_GET_ITEM(out, 0), PyTuple_GET_ITEM(out, 1)};
+        Args o{given, true, a.device};
+        const at::Tensor* q_out = o.tensor(0, at::kBFloat16, {p.B, p.T, p.Hq, p.D});
+        const at::Tensor* k_out = k ? o.tensor(1, at::kBFloat16, {p.B, p.T, p.Hkv, p.D}) : nullptr;
+        if (!o.ok || (!k && given[1] != Py_None)) Py_RETURN_NONE;
+        qo = *q_out;
+        if (k) ko = *k_out;
+    }
     Call c(a.device);
-    at::Tensor qo = empty(q->sizes(), at::kBFloat16, a.device), ko;
-    if (k) ko = empty(k->sizes(), at::kBFloat16, a.device);
+    if (out == Py_None) {
+        qo = empty(q->sizes(), at::kBFloat16, a.device);
+        if (k) ko = empty(k->sizes(), at::kBFloat16, a.device);
+    }
     const int rc = unlocked([&] {
         return lib.rotary(ptr<void>(q), ptr<void>(k), ptr<float>(turn.freqs), ptr<int32_t>(turn.positions), ptr<int32_t>(turn.offsets),
                           ptr<void>(&qo), k ? ptr<void>(&ko) : nullptr, &p, &turn.r, c.stream);
     });
     if (rc != GSD_OK) return PyLong_FromLong(rc);
+    if (out != Py_None) return Py_NewRef(out);
     PyObject* second = k ? THPVariable_Wrap(ko) : Py_NewRef(Py_None);
     return tuple_of({THPVariable_Wrap(qo), second});
     GSD_PY_END
