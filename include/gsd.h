@@ -554,8 +554,8 @@ typedef struct gsd_page_params {
  *                     GSD_ATTN_AUTO, GSD_ATTN_MMA, or GSD_ATTN_TCGEN05 (D == 128 and a group size that divides 128)
  *   c                 host
  * With N = 1 and a mask of one set bit it is ordinary single-token decoding.  Rows at positions >= seq_lens[b] never reach
- * the result whatever the pages hold there, and a row with no visible key yields zeros.  draft_v has to be finite, rows that no
- * node sees among it (their weight is 0, and 0 times an infinity is not).  Weights are rounded to bf16, sums are fp32.
+ * the result whatever the pages hold there, nor do draft rows that no node sees, and a row with no visible key yields zeros.
+ * Weights are rounded to bf16, sums are fp32.
  */
 size_t gsd_verify_attn_paged_workspace_bytes(const gsd_attn_params* p, const gsd_page_params* c);
 int gsd_verify_attn_paged(const void* q, const void* k_pages, const void* v_pages, const int32_t* page_table,

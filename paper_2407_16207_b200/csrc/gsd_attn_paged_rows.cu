@@ -346,6 +346,7 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         bool raise = false;
         if (t >= nPT) {
             const int key0 = (t - nPT) * kKeys;
+            uint32_t seen = 0;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -353,9 +354,19 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
                     const int row = row0 + nt * 8 + 2 * j4 + e;
                     uint32_t w = row < R ? p.mask[((size_t)b * N + row / G) * p.W + (key0 >> 5)] >> (key0 & 16) : 0u;
                     if (N - key0 < kKeys) w &= (1u << (N - key0)) - 1u;
+                    seen |= w;
                     s[nt][e] = (w >> i8) & 1u ? s[nt][e] * p.scale_log2 : -CUDART_INF_F;
                     s[nt][e + 2] = (w >> (i8 + 8)) & 1u ? s[nt][e + 2] * p.scale_log2 : -CUDART_INF_F;
                 }
+            // zeros in the rows of V that no row here sees: their weight is 0, and 0 times an infinity is not
+            uint32_t hide = ~__reduce_or_sync(0xFFFFFFFFu, seen) & (N - key0 < kKeys ? (1u << (N - key0)) - 1u : 0xFFFFu);
+            if (hide != 0) {
+                for (; hide != 0; hide &= hide - 1)
+                    if (lane < D / 8)
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(sv + (lane >> 3) * (kKeys * 128) + (__ffs((int)hide) - 1) * 128 + (lane & 7) * 16), "r"(0) : "memory");
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // (before a copy takes the stage again)
+                __syncwarp();
+            }
         } else {
             const int before = t * kKeys + kKeys - L;       // keys of the last tile that the tile before it has covered, or zeros
             const bool lo = i8 >= before, hi = i8 + 8 >= before;

@@ -597,6 +597,32 @@ __device__ __forceinline__ unsigned unit_live_slice(const TcParams& p, const Uni
     return __reduce_or_sync(0xFFFFFFFFu, live);
 }
 
+// PAGED: draft rows that no node sees must not reach the product with V whatever they hold - their weight is 0, and 0 times an
+// infinity is not.  Usually there are none, since a node sees itself; the draft tiles that have such keys are noted with the unit
+// (bit d; nodes that do not see themselves), and the warp that issues P V works out which are seen by none and clears them there.  (Worked out there for every draft tile it cost 8 x
+// 64/8 heads, N 256, L 4096 35 of 240 us: every instruction of that warp waits for its turn beside the softmax warps.)
+__device__ __forceinline__ uint32_t word_bits(const TcParams& p, int w) {      // the nodes of mask word w
+    const int rem = p.N - 32 * w;
+    return rem >= 32 ? 0xFFFFFFFFu : rem <= 0 ? 0u : (1u << rem) - 1u;
+}
+__device__ __forceinline__ uint32_t unseen_keys(const TcParams& p, int b, int w, int lane) {                 // of mask word w
+    const uint32_t* row = p.mask + (size_t)b * p.N * p.W + w;
+    uint32_t seen = 0;
+    for (int n = lane; n < p.N; n += 32) seen |= row[n * p.W];
+    return ~__reduce_or_sync(0xFFFFFFFFu, seen) & word_bits(p, w);
+}
+__device__ __forceinline__ unsigned unit_hidden(const TcParams& p, const UnitInfo& u, int lane) {
+    const uint32_t* row = p.mask + (size_t)u.b * p.N * p.W;
+    unsigned hidden = 0;
+#pragma unroll 4
+    for (int w = 0; w < p.W; ++w) {
+        const int n = 32 * w + lane;
+        const bool sees_itself = n >= p.N || ((row[(size_t)n * p.W + w] >> lane) & 1u);
+        if (!__all_sync(0xFFFFFFFFu, sees_itself)) hidden |= 1u << (w >> 2);
+    }
+    return hidden;
+}
+
 // Of the draft tiles only the live ones are numbered.
 __device__ __forceinline__ void unit_use_live(UnitInfo& u, unsigned live) {
     u.live = live;
@@ -685,6 +711,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     __shared__ int s_wave_units;                           // one-wave plan: units of the call
     __shared__ UnitInfo s_units[kUnitTable];   // the CTA's first units of work, decoded once up front
     __shared__ unsigned s_live[kThreads / 32]; // live draft tiles in the slices of their mask rows
+    __shared__ unsigned s_hidden[PAGED ? kUnitTable : 1];  // draft tiles with nodes that do not see themselves
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int N = p.N, G = p.G, R = p.R, RT = p.RT;
@@ -890,6 +917,12 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if (part == 0) s_units[k] = u;
             }
         }
+        if (PAGED) {
+            for (int k = me; k < min(n, kUnitTable); k += kDecoders) {
+                const unsigned hidden = unit_hidden(p, unit_base<PLAN>(p, order, PLAN == PLAN_WAVE ? (int)blockIdx.x : unit_index(k), wu), lane);
+                if (lane == 0) s_hidden[k] = hidden;
+            }
+        }
         if (slices > 1) {
             asm volatile("bar.sync 1, %0;" ::"n"(32 * kDecoders) : "memory");
             if (lane == 0 && me < n) {
@@ -907,11 +940,22 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 if (lane == 0) s_units[0] = u;
             }
         }
+        if (PAGED && warp == 1) {
+            const WaveUnit wu = wave_unit(p, blockIdx.x, lane, false);
+            if ((int)blockIdx.x < wu.units) {
+                const unsigned hidden = unit_hidden(p, unit_base<PLAN>(p, order, blockIdx.x, wu), lane);
+                if (lane == 0) s_hidden[0] = hidden;
+            }
+        }
     } else {
         for (int k = warp < 8 ? warp : warp - 1; k < kUnitTable; k += kThreads / 32 - 1) {
             if (k < n_my) {
                 const UnitInfo u = unit_info<PLAN>(p, order, unit_index(k), lane);
                 if (lane == 0) s_units[k] = u;
+                if (PAGED) {
+                    const unsigned hidden = unit_hidden(p, u, lane);
+                    if (lane == 0) s_hidden[k] = hidden;
+                }
             }
         }
     }
@@ -1099,6 +1143,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             const bool two = u.two;
             const int njobs = two ? 2 * u.ntiles : u.ntiles;
             const int n1 = two ? u.ntiles : u.ntiles / 2;      // jobs of stream 1
+            const unsigned hidden = PAGED ? s_hidden[it] : 0u;
             for (int k = 0; k < njobs && ok; ++k) {
                 const int i = k & 1;
                 const int r = kvc + (two ? (k >> 1) : k), st = r % ST;
@@ -1108,6 +1153,22 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
                 const uint32_t tP = tmem + (i ? T::COL_P1 : T::COL_P0), tO = tmem + (i ? T::COL_O1 : T::COL_O0);
                 if (!two || i == 0) {
                     if (!(ok = wait(BAR_V_FULL + st, (r / ST) & 1))) break;
+                }
+                if (PAGED && hidden != 0 && (!two || i == 0)) {
+                    const TileInfo ti = tile_info(u.t_begin + (two ? (k >> 1) : k), u.nPT, u.L, u.live);
+                    if (ti.kind == 2 && ((hidden >> (ti.key0 / BN)) & 1u)) {
+#pragma unroll 1
+                        for (int w = 0; w < BN / 32; ++w) {
+                            uint32_t hide = (ti.key0 >> 5) + w < p.W ? unseen_keys(p, u.b, (ti.key0 >> 5) + w, lane) : 0u;
+                            for (; hide != 0; hide &= hide - 1) {
+                                const int key = 32 * w + __ffs((int)hide) - 1;       // (a lane 16 bytes of its row)
+                                const uint32_t at = sV + (uint32_t)st * TILE_BYTES + (uint32_t)(key >> 3) * (T::BLOCKS * 1024) + (lane >> 3) * 1024 + (key & 7) * 128 + (lane & 7) * 16;
+                                if (lane < 8 * T::BLOCKS) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+                            }
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
                 }
                 if (!(ok = wait(BAR_P_READY + i, par))) break;
                 if (first && (i ? au1 : au) > 0) {

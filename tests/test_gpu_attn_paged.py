@@ -216,3 +216,52 @@ def test_out_is_used_and_the_workspace_is_checked(N):
     # the Python path gives what the extension gives
     same = gsd.gsd_verify_attn_paged(**t, num_splits=np.int64(0))
     assert torch.equal(same, out)
+
+
+@pytest.mark.parametrize("B,Hkv,G,N,D", [(40, 1, 8, 2, 128), (33, 2, 4, 5, 64), (200, 2, 1, 1, 128), (32, 8, 8, 1, 128), (2, 1, 160, 2, 128), (3, 2, 136, 1, 64)])
+@pytest.mark.parametrize("kernel", [0, 1])
+def test_few_rows_in_many_sequences_and_large_groups(B, Hkv, G, N, D, kernel):
+    # more sequences than the plan by length takes, more items than CTAs, groups that the tcgen05 kernel does not take
+    rng = np.random.default_rng([B, G])
+    x = attn_inputs(22, B, N, Hkv * G, Hkv, D, rng.integers(0, 900, B).tolist(), 32)
+    attn_check(x, call(x, kernel=kernel))
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_rows_of_nan_stay_by_themselves(kernel):
+    x = attn_inputs(23, 2, 9, 8, 2, 128, [130, 40], 16)
+    clean = call(x, kernel=kernel)
+    x["q"][1, 4, 3] = float("nan")
+    got = call(x, kernel=kernel)
+    assert got[1, 4, 3].isnan().all()
+    got[1, 4, 3] = clean[1, 4, 3]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_large_scores(kernel):
+    # scores of thousands, of either sign: weights are taken off the row's own maximum
+    x = attn_inputs(24, 2, 20, 8, 2, 128, [200, 33], 16)
+    x["q"] = (x["q"].float() * 64).to(torch.bfloat16)
+    attn_check(x, call(x, kernel=kernel))
+
+
+@pytest.mark.parametrize("fill", [float("nan"), float("inf")])
+@pytest.mark.parametrize("N,Hq,Hkv,D,kernel", [(3, 8, 2, 128, 1), (17, 8, 8, 64, 1), (40, 8, 2, 128, 2), (200, 4, 4, 128, 2), (300, 6, 2, 64, 0), (512, 2, 1, 128, 0), (70, 8, 8, 64, 0), (20, 4, 4, 128, 0)])
+def test_draft_rows_that_no_node_sees(N, Hq, Hkv, D, kernel, fill):
+    # padded nodes, whatever their rows hold; one in the middle and all of the last ones
+    x = attn_inputs(25, 3, N, Hq, Hkv, D, [150, 0, 400], 32)
+    pad = [min(1, N - 1)] + list(range(max(2, N - N // 3), N))
+    x["see"] = x["see"].copy()
+    x["see"][:, :, pad] = False
+    W = x["mask"].shape[2]
+    bits = np.zeros((3, N, W * 32), bool)
+    bits[:, :, :N] = x["see"]
+    if N % 32:
+        bits[:, 0, N:] = True
+    x["mask"] = np.packbits(bits, axis=2, bitorder="little").view(np.int32)
+    clean = call(x, kernel=kernel)
+    attn_check(x, clean)
+    x["dk"][:, pad] = fill
+    x["dv"][:, pad] = fill
+    assert torch.equal(call(x, kernel=kernel), clean)
