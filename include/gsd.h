@@ -583,7 +583,7 @@ int gsd_commit_kv_paged(void* k_pages, void* v_pages, const int32_t* page_table,
  *
  * With one axis that is the position in a text; with three (time, height, width) each pair follows one of them, in blocks or in
  * turns as `axis` says.  The angle is formed and reduced in 64 bits, so that far positions lose nothing; sine, cosine and the
- * rotation are fp32, and the result is rounded to bf16 once.  The columns behind are copied.
+ * rotation are fp32, and the result is rounded to bf16 once; both calls give a row the same bits.  The columns behind are copied.
  */
 #define GSD_ROTARY_HALVES 0       /* pair i: columns i and pairs + i */
 #define GSD_ROTARY_NEIGHBOURS 1   /* pair i: columns 2 i and 2 i + 1 */

@@ -598,9 +598,10 @@ __device__ __forceinline__ unsigned unit_live_slice(const TcParams& p, const Uni
 }
 
 // PAGED: draft rows that no node sees must not reach the product with V whatever they hold - their weight is 0, and 0 times an
-// infinity is not.  Usually there are none, since a node sees itself; the draft tiles that have such keys are noted with the unit
-// (bit d; nodes that do not see themselves), and the warp that issues P V works out which are seen by none and clears them there.  (Worked out there for every draft tile it cost 8 x
-// 64/8 heads, N 256, L 4096 35 of 240 us: every instruction of that warp waits for its turn beside the softmax warps.)
+// infinity is not.  Usually there are none, since a node sees itself; draft tiles with nodes that do not are noted with the unit
+// (bit d), and the warp that issues P V works out which of them are seen by none and clears their rows.  (Worked out there for every
+// draft tile it cost 8 x 64/8 heads, N 256, L 4096 35 of 240 us: every instruction of that warp waits for its turn beside the
+// softmax warps.  With a third of the nodes padding: 244 us; 4 x 40 heads, N 128, L 1024-4096 64.5 instead of 57.4.)
 __device__ __forceinline__ uint32_t word_bits(const TcParams& p, int w) {      // the nodes of mask word w
     const int rem = p.N - 32 * w;
     return rem >= 32 ? 0xFFFFFFFFu : rem <= 0 ? 0u : (1u << rem) - 1u;

@@ -97,6 +97,10 @@ __device__ __forceinline__ uint32_t rotary_pack(float lo, float hi) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// (x, y) turned.  The order of the roundings is fixed, so that a row gets the same bits wherever it is turned.
+__device__ __forceinline__ float turned_x(float x, float y, float c, float s) { return __fmaf_rn(x, c, -__fmul_rn(y, s)); }
+__device__ __forceinline__ float turned_y(float x, float y, float c, float s) { return __fmaf_rn(x, s, __fmul_rn(y, c)); }
+
 // The two pieces of a rotated chunk j, turned.
 template <int D>
 __device__ __forceinline__ void turn_chunk(bool neighbours, const AngleTable<D>& angles, int j, uint4& a, uint4& b) {
@@ -104,15 +108,15 @@ __device__ __forceinline__ void turn_chunk(bool neighbours, const AngleTable<D>&
     if (neighbours) {
         auto turn = [](uint32_t w, float c, float s) {
             const float u = bf16_lo(w), v = bf16_hi(w);
-            return rotary_pack(u * c - v * s, u * s + v * c);
+            return rotary_pack(turned_x(u, v, c, s), turned_y(u, v, c, s));
         };
         a = make_uint4(turn(a.x, c0.x, c0.y), turn(a.y, c0.z, c0.w), turn(a.z, c1.x, c1.y), turn(a.w, c1.z, c1.w));
         b = make_uint4(turn(b.x, c2.x, c2.y), turn(b.y, c2.z, c2.w), turn(b.z, c3.x, c3.y), turn(b.w, c3.z, c3.w));
     } else {
         auto turn = [](uint32_t& x, uint32_t& y, const float4& c) {
             const float u0 = bf16_lo(x), u1 = bf16_hi(x), v0 = bf16_lo(y), v1 = bf16_hi(y);
-            x = rotary_pack(u0 * c.x - v0 * c.y, u1 * c.z - v1 * c.w);
-            y = rotary_pack(u0 * c.y + v0 * c.x, u1 * c.w + v1 * c.z);
+            x = rotary_pack(turned_x(u0, v0, c.x, c.y), turned_x(u1, v1, c.z, c.w));
+            y = rotary_pack(turned_y(u0, v0, c.x, c.y), turned_y(u1, v1, c.z, c.w));
         };
         turn(a.x, b.x, c0);
         turn(a.y, b.y, c1);
