@@ -13,6 +13,7 @@
 #include <Python.h>
 #include <ATen/ATen.h>
 #include <ATen/TensorSubclassLikeUtils.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -122,8 +123,9 @@ struct Args {
 template <class T>
 T* ptr(const at::Tensor* t) { return t ? static_cast<T*>(t->data_ptr()) : nullptr; }
 
+// (at::empty without its way through the dispatcher)
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType dt, int device) {
-    return at::empty(shape, at::TensorOptions().dtype(dt).device(c10::Device(c10::kCUDA, (c10::DeviceIndex)device)));
+    return at::detail::empty_cuda(shape, dt, c10::Device(c10::kCUDA, (c10::DeviceIndex)device), std::nullopt);
 }
 
 // The device made current, its current stream, and the scratch of the call: the caller's or a new one.
@@ -667,7 +669,14 @@ bool turn_args(Args& a, int at, int32_t B, int32_t T, Turn& s) {
     for (int32_t i = 0; i < s.r.pairs; ++i) {
         PyObject* o = PySequence_Fast_GET_ITEM(axes, i);
         int overflow = 0;
-        const long x = PyLong_CheckExact(o) ? PyLong_AsLongAndOverflow(o, &overflow) : -1;
+        long x = -1;
+        if (PyLong_CheckExact(o)) {
+#if PY_VERSION_HEX >= 0x030C0000
+            if (PyUnstable_Long_IsCompact((PyLongObject*)o)) x = (long)PyUnstable_Long_CompactValue((PyLongObject*)o);
+            else
+#endif
+            x = PyLong_AsLongAndOverflow(o, &overflow);
+        }
         if (overflow || x < 0 || x >= (s.positions ? s.r.axes : GSD_ROTARY_MAX_AXES)) return a.ok = false;
         s.r.axis[i] = (uint8_t)x;
         if (x >= s.r.axes) s.r.axes = (int32_t)x + 1;
