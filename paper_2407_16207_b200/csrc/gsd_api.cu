@@ -411,11 +411,16 @@ AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
     pl.dev.splits_a = pl.dev.splits_b = 1;
     const int resident = sm_count * attn_paged_rows_resident(R, p->D);
     const int rounds = ((p->Lmax + 15) / 16 + (p->N + 15) / 16 + 7) / 8;        // of a tile for each warp
+    // Several sequences of up to four rounds are left whole: the merge launch costs more than the cut saves (4 x 64/8 heads, N 1, L 400
+    // 8.4 us cut, 6.5 whole; 2 x 32/8 of 64 7.2 and 5.5; from five rounds on it is the other way round, and for one sequence from
+    // four: 1 x 64/8, N 4, L 400 9.8 and 11.2).
     if (p->num_splits > 0) {
         pl.dev.splits_a = p->num_splits;
-    } else if (pl.items + p->Hkv * pl.dev.tiles_per_unit <= resident && rounds > 2 && p->B > 1 && p->B <= 32) {
-        // the kernel deals the work out by length (which takes it 0.7 us, and one sequence needs none of it); all items of a sequence are cut alike, so with fewer CTAs to spare than a
-        // sequence has items there is nothing to cut
+    } else if (p->B > 1 && rounds <= 4) {
+        pl.dev.splits_a = 1;
+    } else if (pl.items + p->Hkv * pl.dev.tiles_per_unit <= resident && p->B > 1 && p->B <= 32) {
+        // the kernel deals the work out by length (which takes it 0.7 us, and one sequence needs none of it); all items of a sequence
+        // are cut alike, so with fewer CTAs to spare than a sequence has items there is nothing to cut
         pl.dev.balanced = 3;
         pl.ctas = pl.slots = resident;                  // unit w owns slot w
         pl.ws_bytes = plan_part_o_bytes(pl, p->D) + plan_part_ml_bytes(pl) + plan_bal_bytes(pl, p->B);
