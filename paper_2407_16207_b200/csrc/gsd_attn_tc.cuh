@@ -14,7 +14,7 @@
 //   warps 4-7   softmax of stream 1
 //   warp  8     TMA producer (one thread): Q once, then K and V tiles into two smem rings
 //   warp  9     QK^T issuer, warp 11 PV issuer (converged, one elected lane per instruction)
-//   warp 10     TMEM allocation / release
+//   warp 10     TMEM allocation / release; over a cache in pages also the producer of V
 // A stream is a row tile (two row tiles: both streams see every key tile) or, for a unit with
 // one row tile, the even / odd key tiles of that row tile (merged in the epilogue).  A job is
 // one key tile of one stream; jobs alternate between the streams.

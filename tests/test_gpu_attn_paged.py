@@ -265,3 +265,30 @@ def test_draft_rows_that_no_node_sees(N, Hq, Hkv, D, kernel, fill):
     x["dk"][:, pad] = fill
     x["dv"][:, pad] = fill
     assert torch.equal(call(x, kernel=kernel), clean)
+
+
+@pytest.mark.parametrize("name", ["tiny", "llama7b", "llama13b"])
+@pytest.mark.parametrize("page", [16, 128])
+def test_named_configurations_against_the_oracle(name, page):
+    # generated graphs, the padded cache's rows dealt out over pages
+    import gsd_inputs as gi
+    import oracle
+    import paper_2407_16207_b200 as gsd
+    from gpu_util import attn_tensors as padded_tensors, out_to_f64
+    cfg = gi.CONFIGS[name]
+    inp = gi.make_inputs(cfg, accept=False, pad_fill="nan")
+    t = padded_tensors(inp)
+    B, Lmax, Hkv, D = t["k_cache"].shape
+    M = -(-Lmax // page)
+    table = torch.randperm(B * M, generator=torch.Generator().manual_seed(3)).to(torch.int32).view(B, M).cuda()
+    pools = []
+    for n in ("k_cache", "v_cache"):
+        rows = torch.full((B, M * page, Hkv, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+        rows[:, :Lmax] = t[n]
+        pool = torch.empty((B * M, page, Hkv, D), dtype=torch.bfloat16, device="cuda")
+        pool[table.long().flatten()] = rows.view(B * M, page, Hkv, D)
+        pools.append(pool)
+    out = gsd.gsd_verify_attn_paged(t["q"], *pools, table, t["draft_k"], t["draft_v"], t["ancestor_mask"], t["seq_lens"])
+    want = oracle.attn(inp["q"], inp["k_cache"], inp["v_cache"], inp["draft_k"], inp["draft_v"], inp["ancestor_mask"], inp["seq_lens"])
+    err = np.abs(out_to_f64(out) - want)
+    assert err.max() <= 1e-2 and err.mean() <= 1e-3
