@@ -378,19 +378,26 @@ int attn_paged_params_ok(const gsd_attn_params* p, const gsd_page_params* c) {
     }
     return page_rows_log2(c, p->Lmax) < 0 ? GSD_ERR_BAD_SHAPE : GSD_OK;
 }
-// The kernel for few rows reads the cache once for up to 32 rows (48 at D = 64), the tcgen05 kernel for up to 256.  us, few rows and
-// tcgen05; D 128: 1 x 32 heads, L 2048, R = 24 13.9 and 15.8, 32 15.0 and 15.9, 48 15.9 and 16.0, 64 17.9 and 16.1; L 200, R = 48 8.6
-// and 11.5; L 8192, R = 32 30.7 and 32.8, 48 36.4 and 32.9; 8 x 64/8, L 2048-4096, R = 32 28.2 and 29.1, 40 34.6 and 29.9; with more
-// pairs than SMs, 32 x 64/8, L 500-2500, R = 24 44.2 and 45.3, 32 49.2 and 46.7; 8 x 32, L 500-1500, R = 32 36.5 and 33.7.  D 64: 4 x
-// 32/8, L 1000-2000, R = 48 15.1 and 15.9, 64 17.1 and 16.0, L 150-300, R = 32 10.0 and 11.0, 48 12.4 and 11.0; 16 x 32/8, L
-// 1000-2000, R = 32 21.1 and 28.1, 48 26.2 and 28.4, 64 31.2 and 28.5.
+// Rounds of keys, a tile of 16 for each warp, that the longest sequence can take in the kernel for few rows.
+int attn_paged_rounds(const gsd_attn_params* p) { return ((p->Lmax + 15) / 16 + (p->N + 15) / 16 + 7) / 8; }
+
+// The kernel for few rows reads the cache once for up to 32 rows (24 at D = 64), the tcgen05 kernel for up to 256; a launch of the
+// former is over sooner.  So it gets the rows that it reads the cache once for (48 at D = 64, which L2 feeds, unless pairs and keys are
+// many), and more where its items run side by side and are short.  us, few rows and tcgen05, L between half and all of the length
+// given.  D 128: 1 x 32/8 heads, R = 128, L 2000 12.8 and 12.9, L 4000 17.7 and 13.8; 4 x 32/8, R = 64, L 500 9.2 and 11.8, L 2000
+// 17.2 and 17.2, L 8000 35.5 and 28.7, R = 32, L 8000 27.7 and 28.3; 16 x 32/8, R = 32, L 8000 85.1 and 84.3, R = 40, L 500 19.9 and
+// 14.1; 48 x 32/8, L 2000, R = 24 62 and 63, R = 32 69 and 64.  D 64: 4 x 32/8, R = 96, L 1000 12.0 and 15.8, L 4000 23.3 and 20.1;
+// 16 x 32/8, R = 48, L 8000 66 and 73, R = 64, L 500 18.9 and 14.0; 48 x 32/8, R = 32, L 4000 82 and 87, R = 48 92 and 87.
 int attn_paged_pick_kernel(const gsd_attn_params* p, int sm_count) {
     if (p->kernel != GSD_ATTN_AUTO) return p->kernel;
-    const int G = p->Hq / p->Hkv, R = p->N * G, pairs = p->B * p->Hkv;
+    const int G = p->Hq / p->Hkv, rounds = attn_paged_rounds(p);
+    const long long R = (long long)p->N * G, pairs = (long long)p->B * p->Hkv;
     if (!attn_tcgen05_supports(p->D, G)) return GSD_ATTN_MMA;
+    const int once = p->D == 64 ? 24 : 32, side_by_side = sm_count * attn_paged_rows_resident(once, p->D);
     bool few;
-    if (p->D == 64) few = R <= 32 || (R <= 48 && p->Lmax >= 512);
-    else few = R <= 24 || (R <= 32 && pairs <= sm_count) || (R <= 48 && 2 * pairs <= sm_count && p->Lmax <= 2048);
+    if (p->D == 64) few = R <= 32 || (R <= 48 && (pairs <= sm_count || rounds <= 8));
+    else few = R <= 24 || (R <= 32 && pairs <= sm_count);
+    few = few || (R <= 128 && (R + once - 1) / once * pairs <= side_by_side && R * rounds <= (8 * pairs <= sm_count ? 2048 : 1024));
     return few ? GSD_ATTN_MMA : GSD_ATTN_TCGEN05;
 }
 AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
@@ -403,20 +410,23 @@ AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
     AttnPlan pl = {};
     const int R = p->N * (p->Hq / p->Hkv);
     pl.kernel = GSD_ATTN_MMA;
-    pl.rows_per_item = attn_paged_rows(R, p->D);
+    const int rounds = attn_paged_rounds(p);
+    pl.rows_per_item = attn_paged_rows(R, p->D, p->B * p->Hkv, p->num_splits > 0 ? p->num_splits : (rounds + 19) / 20, sm_count);
     pl.part_rows = 64;
     pl.dev.tiles_per_unit = (R + pl.rows_per_item - 1) / pl.rows_per_item;
     pl.items = pl.dev.tiles_per_unit * p->B * p->Hkv;
     pl.dev.items_a = pl.items;
     pl.dev.splits_a = pl.dev.splits_b = 1;
-    const int resident = sm_count * attn_paged_rows_resident(R, p->D);
-    const int rounds = ((p->Lmax + 15) / 16 + (p->N + 15) / 16 + 7) / 8;        // of a tile for each warp
-    // Several sequences of up to four rounds are left whole: the merge launch costs more than the cut saves (4 x 64/8 heads, N 1, L 400
-    // 8.4 us cut, 6.5 whole; 2 x 32/8 of 64 7.2 and 5.5; from five rounds on it is the other way round, and for one sequence from
-    // four: 1 x 64/8, N 4, L 400 9.8 and 11.2).
+    const int resident = sm_count * attn_paged_rows_resident(pl.rows_per_item, p->D);
+    // A cut has to save more than the merge launch and its partial results cost, about eight rounds on the longest sequence (five for
+    // a single one, which needs no plan by length).  us cut and whole, D 128: 4 x 32/8 heads, N 2, L 250-500 8.4 and 6.6, L 500-1000 9.4
+    // and 9.1, L 1000-2000 11.8 and 12.9; 1 x 32/8, N 4, L 250-500 6.4 and 6.3, L 500-1000 6.5 and 8.1; 8 x 32/8, N 2, L 1000-2000 15.3
+    // and 13.8.  Past 16 rounds lengths may differ by so much that several sequences are cut wherever an SM is left.
+    const long long gain = (long long)rounds * std::max(sm_count - pl.items, 0);
+    const bool cut = p->B > 1 ? gain >= 8 * sm_count || (rounds > 16 && gain > 0) : gain >= 5 * sm_count;
     if (p->num_splits > 0) {
         pl.dev.splits_a = p->num_splits;
-    } else if (p->B > 1 && rounds <= 4) {
+    } else if (!cut) {
         pl.dev.splits_a = 1;
     } else if (pl.items + p->Hkv * pl.dev.tiles_per_unit <= resident && p->B > 1 && p->B <= 32) {
         // the kernel deals the work out by length (which takes it 0.7 us, and one sequence needs none of it); all items of a sequence

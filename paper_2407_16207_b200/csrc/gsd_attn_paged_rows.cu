@@ -49,7 +49,7 @@ struct RowsGeo {
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int ROWS = 8 * NT;                         // stacked rows of an item
     static constexpr int TILE = kKeys * D * 2;                  // bytes of a K or V tile
-    static constexpr int BLOCKS = D == 64 && NT <= 2 ? 2 : 1;   // CTAs an SM
+    static constexpr int BLOCKS = D == 64 && NT <= 3 ? 2 : 1;   // CTAs an SM
     static constexpr int STAGES = D == 128 ? 3 : BLOCKS == 2 ? 3 : 5;
     static constexpr int RING = WARPS * STAGES * 2 * TILE;
     static constexpr int MTILES = D / 16;                       // output tiles of 16 columns
@@ -540,14 +540,23 @@ int launch_t(const AttnArgs& a) {
 
 }  // namespace
 
-// Stacked rows of an item: as few items as 32 rows each (48 at D = 64, whose accumulators are half as wide) allow, with the row
-// groups shared out evenly.
-int attn_paged_rows(int R, int D) {
-    const int most = D == 64 ? 48 : 32, items = (R + most - 1) / most, groups = (R + 7) / 8;
-    const int even = (groups + items - 1) / items;
-    return 8 * (even > 4 ? (even + 1) / 2 * 2 : even);
+// Stacked rows of an item.  More rows an item read the cache fewer times (the rest comes from L2); fewer rows spread the same
+// work over more SMs, and a warp's round is shorter.  So an item gets the fewest rows with which all items, each cut into as many
+// ranges as the length asks for (one for 20 rounds of keys), still run side by side: up to 32 rows with a CTA an SM; for D = 64,
+// where two fit, up to 24 rows with two; past that the most rows.  us at 8, 16, 24 and 32 rows, D 128: 4 x 32/8 heads, N 8, L
+// 250-500 6.9, 9.2, 9.2, 12.3, L 4000-8000 36, 26, 26, 28; 1 x 32/8, N 12, L 1000 7.6, 8.2, 9.1, 9.1; 16 x 32/8, N 16, L 500-1000
+// 56, 40, 36, 30.  D 64: 4 x 96/24, N 16, L 250-500 27, 15, 12, 18; 48 x 32/8, N 16, L 100-200 55, 35, 31, 43.
+int attn_paged_rows(int R, int D, int pairs, int ranges, int sm_count) {
+    const int groups = (R + 7) / 8;
+    for (int ctas = 1; ctas <= (D == 64 ? 2 : 1); ++ctas)
+        for (int per = 1; per <= (ctas == 1 ? 4 : 3); ++per) {
+            const int items = (groups + per - 1) / per;
+            if ((long long)pairs * items * ranges <= (long long)sm_count * ctas) return 8 * ((groups + items - 1) / items);
+        }
+    const int most = D == 64 ? 3 : 4, items = (groups + most - 1) / most;
+    return 8 * ((groups + items - 1) / items);
 }
-int attn_paged_rows_resident(int R, int D) { return D == 64 && attn_paged_rows(R, D) <= 16 ? 2 : 1; }
+int attn_paged_rows_resident(int rows, int D) { return D == 64 && rows <= 24 ? 2 : 1; }
 
 int launch_attn_paged_rows(const AttnArgs& a) {
     switch (a.plan.rows_per_item * 1000 + a.D) {
@@ -559,7 +568,6 @@ int launch_attn_paged_rows(const AttnArgs& a) {
         case 16064: return launch_t<64, 2>(a);
         case 24064: return launch_t<64, 3>(a);
         case 32064: return launch_t<64, 4>(a);
-        case 48064: return launch_t<64, 6>(a);
     }
     return GSD_ERR_BAD_SHAPE;
 }

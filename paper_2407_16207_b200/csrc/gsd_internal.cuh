@@ -223,8 +223,8 @@ int launch_attn_q8_mma(const AttnArgs& a);
 // zeros for rows that no node sees.
 int launch_kv8_expand(const AttnArgs& a, void* k_out, void* v_out, void* draft_v_out);
 int launch_attn_paged_rows(const AttnArgs& a);
-int attn_paged_rows(int R, int D);            // stacked rows of one of its items
-int attn_paged_rows_resident(int R, int D);   // its CTAs an SM holds
+int attn_paged_rows(int R, int D, int pairs, int ranges, int sm_count);            // stacked rows of one of its items
+int attn_paged_rows_resident(int rows, int D);   // its CTAs an SM holds
 int attn_q8_mma_rows(int R);                  // stacked rows of one of its items
 int attn_q8_mma_resident(int R, int D);              // its CTAs an SM holds
 int launch_attn_tcgen05(const AttnArgs& a);

@@ -63,6 +63,21 @@ def test_many_items(page, B, Hkv, G, N):
     attn_check(x, call(x))
 
 
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("B,Hkv,G,N", [(1, 2, 4, 30), (3, 4, 4, 17), (5, 8, 4, 12), (12, 8, 1, 32), (10, 10, 3, 11), (33, 3, 5, 9), (40, 6, 4, 13)])
+@pytest.mark.parametrize("longest", [250, 2600])
+def test_items_of_every_size(B, Hkv, G, N, D, longest):
+    # as the pairs grow in number, their rows are shared out among fewer items; left whole, cut alike and cut by length
+    rng = np.random.default_rng([B, N])
+    lens = rng.integers(0, 200, B)
+    lens[B // 2] = longest
+    x = attn_inputs(11, B, N, Hkv * G, Hkv, D, lens.tolist(), 32)
+    out = call(x, kernel=1)
+    attn_check(x, out)
+    attn_check(x, call(x))
+    assert torch.equal(out, call(x, kernel=1))
+
+
 @pytest.mark.parametrize("kernel", [1, 2])
 def test_rows_that_see_nothing_are_zero(kernel):
     x = attn_inputs(5, 2, 11, 8, 2, 128, [0, 40], 16, mask="none")
