@@ -71,7 +71,7 @@ int attn_pick_kernel(const gsd_attn_params* p, int sm_count) {
 }
 
 AttnPlan attn_make_plan(const gsd_attn_params* p, int sm_count, bool by_length) {
-    AttnPlan pl;
+    AttnPlan pl = {};
     pl.kernel = attn_pick_kernel(p, sm_count);
     const bool tc = pl.kernel == GSD_ATTN_TCGEN05;
     const int G = p->Hq / p->Hkv;
@@ -424,8 +424,24 @@ AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
     // and 13.8.  Past 16 rounds lengths may differ by so much that several sequences are cut wherever an SM is left.
     const long long gain = (long long)rounds * std::max(sm_count - pl.items, 0);
     const bool cut = p->B > 1 ? gain >= 8 * sm_count || (rounds > 16 && gain > 0) : gain >= 5 * sm_count;
+    // A cluster for each item of several sequences, its CTAs taking even shares of the keys: no plan by length, no merge launch, but a
+    // range is as long as its sequence's share, at most 20 rounds here, so that lengths that differ cost little.  us by length and in
+    // clusters: D 128, N 1, 4 x 32/8 heads, L 500-1000 9.0 and 8.5, 8 x 64/8, L 1000-2000 15.4 and 14.1, L 2000-4000 23.2 and 21.4, L
+    // 100-4000 17.3 and 16.6; D 64, N 1, 4 x 32/8, L 1000-2000 9.8 and 8.5, 16 x 32/2, L 100-4000 11.5 and 12.5.  Items of 16 rows and
+    // more gain nothing on average (N 4, 8 x 64/8, L 2000-4000 28.2 and 27.0, L 100-4000 22.0 and 24.6), nor does a single sequence, which
+    // has no plan.  Nine tenths of the SMs can be filled with clusters of up to five, three quarters with larger ones: 16 clusters of
+    // eight did not run side by side (12.1 us, of six 7.2).  Where few of them fill less than that, the plan by length has more SMs (48
+    // items, L 2000-4000 13.1 and 14.2 us).
+    int cs = sm_count * 9 / (10 * pl.items);
+    if (cs > 5) cs = std::min(8, sm_count * 3 / (4 * pl.items));
+    const bool clusters = p->B > 1 && pl.rows_per_item == 8 && cs >= 2 && (cs > 5 || 4 * cs * pl.items >= 3 * sm_count) &&
+                          rounds * (cs - 1) >= 5 * cs && rounds <= 20 * cs;
     if (p->num_splits > 0) {
         pl.dev.splits_a = p->num_splits;
+    } else if (clusters) {
+        pl.cluster = pl.dev.splits_a = cs;
+        pl.ctas = pl.items * cs;
+        return pl;
     } else if (!cut) {
         pl.dev.splits_a = 1;
     } else if (pl.items + p->Hkv * pl.dev.tiles_per_unit <= resident && p->B > 1 && p->B <= 32) {

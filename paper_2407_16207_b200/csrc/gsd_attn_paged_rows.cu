@@ -12,10 +12,12 @@
 // 2^kLag: the weights are rounded to bf16, whose relative step does not depend on their size, and sums stay fp32.
 //
 // The work is dealt out by length inside the kernel for up to 32 sequences: every item (a group of rows of a sequence and
-// kv head) is cut into ranges of at most T rounds of keys, T the least with which all ranges are resident at once.
+// kv head) is cut into ranges of at most T rounds of keys, T the least with which all ranges are resident at once; a merge pass brings
+// them together.  Where items of eight rows are cut evenly and not too long, a cluster has the ranges of an item and needs no such pass.
 //
 // Bound by DRAM where keys are many, by dependent trips and the length of a warp's round where they are few.  32 x 64/8 heads of 128,
-// N 1, L 4096: 83 us for 537 MB, the rate of a copy; 8 of them, L 1500-3500, 19.8 us for 74 MB with the merge launch (padded cache 24.0).
+// N 1, L 4096: 83 us for 537 MB, the rate of a copy; 8 of them, L 1500-3500, 18.4 us for 74 MB in clusters of two (by length, with the
+// merge launch, 20.1; padded cache 24.1).
 // 4 x 32/8 heads of 64, N 12, L 1000-4000 15.9 us (16.2).  Four warps and two CTAs an SM, or two and four, take 92 and 97 us for the
 // first; copies by cp.async 84 us; weights in two bf16 terms bring the error from 2.3e-3 to 1.7e-3 for 1-5 % of the time.
 #include "gsd_tma.cuh"
@@ -43,6 +45,7 @@ struct RowsParams {
     int32_t* status;
     int B, N, Hq, Hkv, Lmax, G, W, R;
     int slots;
+    int cluster;             // the ranges of an item are brought together by a cluster of as many CTAs; 0: by the merge pass, or whole
     float scale_log2;
     unsigned long long wait_limit_ns;
     int withhold_first_k;    // test hook: every warp leaves out the K copy of its first tile
@@ -60,7 +63,8 @@ struct RowsGeo {
     static constexpr int MTILES = D / 16;                       // output tiles of 16 columns
     static constexpr int VALUES = MTILES * 4 + 4;               // of a lane and 8 rows, when the warps' results are brought together
     static constexpr int MEET = WARPS * NT * VALUES * 32 * 4;
-    static constexpr int Q_AT = RING > MEET ? RING : MEET;      // query fragments: [row group][k-step][lane] pairs of registers
+    static constexpr int SHARED = NT == 1 ? ROWS * (D + 4) * 4 : 0;     // what a CTA of a cluster has of its item: [row][D + 4], behind MEET
+    static constexpr int Q_AT = RING > MEET + SHARED ? RING : MEET + SHARED;    // query fragments: [row group][k-step][lane] pairs of registers
     static constexpr int SMEM = Q_AT + NT * (D / 16) * 32 * 8 + 1024;       // (alignment)
 };
 
@@ -109,6 +113,28 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, unsigne
         ok = __all_sync(0xFFFFFFFFu, ok);
     }
     return ok;
+}
+
+constexpr int kMostCluster = 8;
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+// From the shared memory of CTA k of the cluster, at this CTA's address `at`.
+__device__ __forceinline__ uint32_t of_cta(uint32_t at, int k) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(k));
+    return r;
+}
+__device__ __forceinline__ float2 ld_cluster2(uint32_t at, int k) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(of_cta(at, k)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t at, int k) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(of_cta(at, k)) : "memory");
+    return v;
 }
 
 // What a CTA works on: rows of (sequence b, kv head c), keys of one of `nsplit` ranges.
@@ -448,6 +474,7 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     }
 
     // ---- the warps' results meet in the memory of the rings
+    float* const shared = reinterpret_cast<float*>(smem + T::MEET);     // for the cluster: a row's sums, then m and l
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -501,12 +528,45 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
             const float inv = l > 0.f ? 1.f / l : 0.f;
             *reinterpret_cast<uint2*>(p.out + (((size_t)b * N + row / G) * p.Hq + c * G + row % G) * D + col) =
                 make_uint2(pack_bf16(r[0] * inv, r[1] * inv), pack_bf16(r[2] * inv, r[3] * inv));
+        } else if (NT == 1 && p.cluster) {
+            float* at = shared + (nt * 8 + r8) * (D + 4);
+            *reinterpret_cast<float4*>(at + col) = make_float4(r[0], r[1], r[2], r[3]);
+            if (quad == 0) *reinterpret_cast<float2*>(at + D) = make_float2(m, l);
         } else {
             if (!GSD_IN_BOUNDS(u.slot >= 0 && u.slot < p.slots, p.status)) continue;
             *reinterpret_cast<float4*>(p.part_o + (((size_t)u.slot * (D / 4) + quad) * 64 + nt * 8 + r8) * 4) = make_float4(r[0], r[1], r[2], r[3]);
             if (quad == 0) *reinterpret_cast<float2*>(p.part_ml + ((size_t)u.slot * 64 + nt * 8 + r8) * 2) = make_float2(m, l);
         }
     }
+    if (NT != 1 || p.cluster == 0) return;
+    // ---- the ranges meet: each CTA of the cluster takes a share of the rows' columns
+    cluster_meet();
+    const uint32_t mine = smem_u32(shared);
+    for (int x = u.split * T::THREADS + tid; x < T::ROWS * (D / 4); x += p.cluster * T::THREADS) {
+        const int r = x / (D / 4), col = x % (D / 4) * 4, row = row0 + r;
+        if (row >= R || !GSD_IN_BOUNDS(b < p.B && c < p.Hkv, p.status)) continue;
+        float m = -CUDART_INF_F, l = 0.f;
+        float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
+        float2 ml[kMostCluster];
+#pragma unroll
+        for (int k = 0; k < kMostCluster; ++k) {
+            ml[k] = k < p.cluster ? ld_cluster2(mine + (r * (D + 4) + D) * 4, k) : make_float2(-CUDART_INF_F, 0.f);
+            m = fmaxf(m, ml[k].x);
+        }
+        const float m_use = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+        for (int k = 0; k < kMostCluster; ++k) {
+            if (k >= p.cluster) break;
+            const float wk = fast_exp2(ml[k].x - m_use);
+            const float4 v = ld_cluster4(mine + (r * (D + 4) + col) * 4, k);
+            l += wk * ml[k].y;
+            o4.x += wk * v.x; o4.y += wk * v.y; o4.z += wk * v.z; o4.w += wk * v.w;
+        }
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        *reinterpret_cast<uint2*>(p.out + (((size_t)b * N + row / G) * p.Hq + c * G + row % G) * D + col) =
+            make_uint2(pack_bf16(o4.x * inv, o4.y * inv), pack_bf16(o4.z * inv, o4.w * inv));
+    }
+    cluster_meet();                         // (no CTA ends while another reads its memory)
 }
 
 template <int D, int NT>
@@ -524,7 +584,7 @@ int launch_t(const AttnArgs& a) {
     p.withhold_first_k = g_withhold_first_k;
     p.mask = a.mask; p.seq_lens = a.seq_lens; p.out = (__nv_bfloat16*)a.out; p.status = a.status;
     p.B = a.B; p.N = a.N; p.Hq = a.Hq; p.Hkv = a.Hkv; p.Lmax = a.Lmax; p.G = a.G; p.W = a.W; p.R = a.N * a.G;
-    p.scale_log2 = a.scale_log2; p.plan = a.plan.dev; p.slots = a.plan.slots;
+    p.scale_log2 = a.scale_log2; p.plan = a.plan.dev; p.slots = a.plan.slots; p.cluster = a.plan.cluster;
     p.part_o = (float*)a.workspace;
     p.part_ml = (float*)((char*)a.workspace + plan_part_o_bytes(a.plan, a.D));
     p.left = a.plan.dev.balanced == 3 ? plan_left_table(a.plan, a.D, a.workspace) : nullptr;
@@ -539,7 +599,18 @@ int launch_t(const AttnArgs& a) {
             if (dev >= 0 && dev < 64) done[dev] = true;
         }
     }
-    GSD_CUDA_TRY(launch_dependent(attn_paged_rows_kernel<D, NT>, dim3(a.plan.ctas), dim3(RowsGeo<D, NT>::THREADS), smem, a.stream, tk, tv, tdk, tdv, p));
+    cudaLaunchAttribute attr[2];
+    dependent_launch_attr(attr);
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = a.plan.cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.plan.ctas);
+    cfg.blockDim = dim3(RowsGeo<D, NT>::THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = a.stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.plan.cluster > 0 ? 2 : 1;
+    GSD_CUDA_TRY(cudaLaunchKernelEx(&cfg, attn_paged_rows_kernel<D, NT>, tk, tv, tdk, tdv, p));
     return GSD_OK;
 }
 

@@ -94,7 +94,8 @@ struct AttnPlan {
     int part_rows;      // rows of a partial-result slot: 64 or 2 x 128
     int items;
     int ctas;
-    int slots;          // partial-result slots; 0 when nothing is split
+    int slots;          // partial-result slots; 0 when nothing is split, or split among the CTAs of a cluster
+    int cluster;        // CTAs of a cluster, the ranges of an item (attn_paged_rows_kernel); 0: no clusters
     PlanDev dev;
     size_t ws_bytes;
 };

@@ -78,6 +78,31 @@ def test_items_of_every_size(B, Hkv, G, N, D, longest):
     assert torch.equal(out, call(x, kernel=1))
 
 
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("B,Hkv,G,N", [(2, 8, 4, 2), (3, 4, 7, 1), (4, 8, 1, 8), (8, 8, 8, 1), (5, 3, 3, 2), (9, 1, 5, 1), (30, 2, 2, 3), (20, 2, 4, 2), (13, 2, 8, 1)])
+def test_ranges_of_a_cluster(B, Hkv, G, N, D):
+    # a cluster of two to eight CTAs an item: no workspace; none of the keys, one, a range without any, a page that is not there
+    import paper_2407_16207_b200 as gsd
+    rng = np.random.default_rng([B, Hkv, N])
+    lens = rng.integers(0, 1800, B)
+    lens[0], lens[1], lens[-1] = 0, 1, 1800
+    x = attn_inputs(12, B, N, Hkv * G, Hkv, D, lens.tolist(), 32)
+    assert gsd.gsd_verify_attn_paged_workspace_bytes(B, N, Hkv * G, Hkv, D, 32, x["table"].shape[1]) == 0
+    out = call(x)
+    attn_check(x, out)
+    assert torch.equal(out, call(x))
+    attn_check(x, call(x, num_splits=3))
+    x["table"][-1, 20] = x["k"].shape[0]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = gsd.gsd_verify_attn_paged(**attn_tensors(x), status=status)
+    assert int(status.item()) == 0x1000
+    x["table"][-1, 20] = 0
+    x["k"] = torch.cat([x["k"], torch.zeros_like(x["k"][:1])])
+    x["v"] = torch.cat([x["v"], torch.zeros_like(x["v"][:1])])
+    x["table"][-1, 20] = x["k"].shape[0] - 1
+    attn_check(x, out)
+
+
 @pytest.mark.parametrize("kernel", [1, 2])
 def test_rows_that_see_nothing_are_zero(kernel):
     x = attn_inputs(5, 2, 11, 8, 2, 128, [0, 40], 16, mask="none")
