@@ -533,7 +533,7 @@ int gsd_append_kv_q8(void* k_cache, void* v_cache, int8_t* k_exp, int8_t* v_exp,
  *
  * `page` is 16, 32, 64, 128 or 256 rows; any number of pages the memory holds.  Several sequences may read the same pages (a
  * common system prompt); a page that a call writes must not be named twice in what it reads or writes.  Only the entries that
- * hold a visible row or get a new one are read, the rest of the table may be anything.  An entry outside [0, num_pages) among
+ * hold a visible row or get a new one count, the rest of the table may be anything.  An entry outside [0, num_pages) among
  * those never leads to an access: gsd_verify_attn_paged takes its rows for zeros, the writers drop the rows from the first
  * without a page on, and GSD_DEV_BAD_PAGE says so.
  */

@@ -16,7 +16,7 @@
 // them together.  Where items of eight rows are cut evenly and not too long, a cluster has the ranges of an item and needs no such pass.
 //
 // Bound by DRAM where keys are many, by dependent trips and the length of a warp's round where they are few.  32 x 64/8 heads of 128,
-// N 1, L 4096: 83 us for 537 MB, the rate of a copy; 8 of them, L 1500-3500, 18.4 us for 74 MB in clusters of two (by length, with the
+// N 1, L 4096: 83 us for 537 MB, the rate of a copy; 8 of them, L 1500-3500, 17.9 us for 74 MB in clusters of two (by length, with the
 // merge launch, 20.1; padded cache 24.1).
 // 4 x 32/8 heads of 64, N 12, L 1000-4000 15.9 us (16.2).  Four warps and two CTAs an SM, or two and four, take 92 and 97 us for the
 // first; copies by cp.async 84 us; weights in two bf16 terms bring the error from 2.3e-3 to 1.7e-3 for 1-5 % of the time.
@@ -211,7 +211,9 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     __shared__ __align__(8) unsigned long long s_full[WARPS * ST];
     unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
 
-    if (p.slots > 0) let_successor_start();
+    // (Where an SM holds two CTAs, the next call's would take places beside this one's: 11.3 -> 19.3 us for 4 x 32/8 heads of 64, N 8, L
+    // 1000-2000.  With one they do not fit, and a chain of short calls is a seventh faster: 1 x 32/8 of 128, L 60-120 4.5 -> 3.8.)
+    if (p.slots > 0 || T::BLOCKS == 1) let_successor_start();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int i8 = lane >> 2, j4 = lane & 3;
     const int N = p.N, G = p.G, R = p.R;
@@ -227,6 +229,16 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
     }
     __syncwarp();
     Unit u;
+    const bool by_length = p.plan.balanced == 3;
+    if (!by_length) {
+        // (no need to wait for what precedes the call)
+        int item;
+        plan_decode(p.plan, blockIdx.x, item, u.split, u.nsplit, u.slot);
+        const int pair = item / p.plan.tiles_per_unit;   // b * Hkv + c
+        u.row0 = item - pair * p.plan.tiles_per_unit;
+        u.b = pair / p.Hkv;
+        u.c = pair - u.b * p.Hkv;
+    }
     wait_for_predecessor();
     if (tid < kTableLines) {
         // the table's first lines, a few a CTA, while the lengths come: its look-ups are the next trip
@@ -235,44 +247,53 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         if (row < p.B && at < p.pages.max_pages)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(p.pages.table + (size_t)row * p.pages.max_pages + at) : "memory");
     }
-    if (p.plan.balanced == 3) {
-        if (!unit_by_length<WARPS>(p, blockIdx.x, lane, blockIdx.x == 0 && warp == 0, u)) return;
-    } else {
-        int item;
-        plan_decode(p.plan, blockIdx.x, item, u.split, u.nsplit, u.slot);
-        const int pair = item / p.plan.tiles_per_unit;   // b * Hkv + c
-        u.row0 = item % p.plan.tiles_per_unit;
-        u.b = pair / p.Hkv;
-        u.c = pair % p.Hkv;
-        u.L = visible_len(p, u.b);
-    }
+    if (by_length && !unit_by_length<WARPS>(p, blockIdx.x, lane, blockIdx.x == 0 && warp == 0, u)) return;
     u.row0 *= T::ROWS;
-    const int b = u.b, c = u.c, row0 = u.row0, L = u.L;
-    if (tid == 0 && p.status) {
-        const int given = p.seq_lens[b];
-        if (given < 0 || given > p.Lmax) atomicOr((unsigned*)p.status, GSD_DEV_BAD_SEQ_LEN);
+    const int b = u.b, c = u.c, row0 = u.row0;
+    // Key tiles of 16: the prefix, then the draft block.  By length the CTA has a run of them, a warp every WARPS-th of the run; else
+    // the warps of all ranges take them in turns, so that which tiles a warp begins with does not hang on the length.
+    const int step = by_length ? WARPS : WARPS * u.nsplit;
+    const int32_t* table = p.pages.table + (size_t)b * p.pages.max_pages;
+    const int given = by_length ? 0 : p.seq_lens[b];
+    // What the table has for the warp's tiles `lane`, and the query rows (a warp for every eight), are asked for beside the length, a
+    // trip to memory less.  Queries before keys: behind 128 KB of them an SM they took 2.5 us.
+    const int entry = by_length ? 0 : table[min((u.split * WARPS + warp + lane * step) * kKeys >> p.pages.page_log2, p.pages.max_pages - 1)];
+    static_assert(NT <= WARPS, "a row group a warp");
+    uint32_t qw[KS][2];
+    if (warp < NT) {
+        const int row = row0 + warp * 8 + i8;
+        const bool in = row < R;
+        const int rr = in ? row : 0;
+        const __nv_bfloat16* q = p.q + (((size_t)b * N + rr / G) * p.Hq + c * G + rr % G) * D + 2 * j4;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qw[ks][0] = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16) : 0u;
+            qw[ks][1] = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16 + 8) : 0u;
+        }
     }
-    // Key tiles of 16: the prefix, then the draft block.  The CTA has [t_begin, t_end) of them, a warp every WARPS-th.
+    const int L = by_length ? u.L : min(max(given, 0), p.Lmax);
+    if (tid == 0 && p.status) {
+        const int len = by_length ? p.seq_lens[b] : given;
+        if (len < 0 || len > p.Lmax) atomicOr((unsigned*)p.status, GSD_DEV_BAD_SEQ_LEN);
+    }
     const int nPT = (L + kKeys - 1) / kKeys, nT = nPT + (N + kKeys - 1) / kKeys;
-    const int per = ((nT + WARPS - 1) / WARPS + u.nsplit - 1) / u.nsplit * WARPS;
-    const int t_begin = min(u.split * per, nT), t_end = min(t_begin + per, nT);
-    const int first = t_begin + warp;
-    const int n_tiles = max(0, (t_end - first + WARPS - 1) / WARPS);
+    const int per = by_length ? ((nT + WARPS - 1) / WARPS + u.nsplit - 1) / u.nsplit * WARPS : WARPS;
+    const int first = u.split * per + warp, t_end = by_length ? min(u.split * per + per, nT) : nT;
+    const int all_tiles = max(0, t_end - first + step - 1), n_tiles = step == WARPS ? all_tiles / WARPS : all_tiles / step;    // (a shift)
 
     // ---- the ring: K and V tiles of 16 rows, blocks of 64 columns
     const uint32_t ring = smem_u32(smem) + warp * (ST * 2 * T::TILE);
-    const int32_t* table = p.pages.table + (size_t)b * p.pages.max_pages;
     // the pages of the warp's tiles i0 + lane; -1: none (draft tiles, no such tile, no such page)
     auto find_pages = [&](int i0) -> int {
-        const int key = (first + (i0 + lane) * WARPS) * kKeys;
+        const int key = (first + (i0 + lane) * step) * kKeys;
         if (i0 + lane >= n_tiles || key >= L || !GSD_IN_BOUNDS(key >> p.pages.page_log2 < p.pages.max_pages, p.status)) return -1;
-        const int page = table[key >> p.pages.page_log2];
+        const int page = i0 == 0 && !by_length ? entry : table[key >> p.pages.page_log2];
         if ((unsigned)page < (unsigned)p.pages.num_pages) return page;
         if (p.status) atomicOr((unsigned*)p.status, GSD_DEV_BAD_PAGE);
         return -1;
     };
     auto issue = [&](int i, int stage, int pages) {
-        const int t = first + i * WARPS;
+        const int t = first + i * step;
         const int page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
         if (lane == 0) {
             const uint32_t dst = ring + stage * (2 * T::TILE), bar = full + 8 * stage;
@@ -290,26 +311,12 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
         }
         __syncwarp();
     };
-    // The query rows, asked for before the keys fill the queues (behind 128 KB of them an SM they took 2.5 us): a warp for every
-    // eight rows.
-    static_assert(NT <= WARPS, "a row group a warp");
-    uint32_t qw[KS][2];
-    if (warp < NT) {
-        const int row = row0 + warp * 8 + i8;
-        const bool in = row < R;
-        const int rr = in ? row : 0;
-        const __nv_bfloat16* q = p.q + (((size_t)b * N + rr / G) * p.Hq + c * G + rr % G) * D + 2 * j4;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            qw[ks][0] = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16) : 0u;
-            qw[ks][1] = in ? *reinterpret_cast<const uint32_t*>(q + ks * 16 + 8) : 0u;
-        }
-    }
-    int pages = find_pages(0), pages_next = find_pages(32);
+    int pages = find_pages(0);
     for (int s = 0; s < min(ST, n_tiles); ++s) issue(s, s, pages);
+    int pages_next = find_pages(32);
 
     // the mask words of the draft tiles, which come last, as a trip of their own
-    for (int t = max(first, nPT); t < t_end; t += WARPS)
+    for (int t = first + (n_tiles - 1) * step; t >= max(first, nPT); t -= step)
         for (int node = row0 / G + lane; node <= min(row0 + T::ROWS - 1, R - 1) / G; node += 32)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(p.mask + ((size_t)b * N + node) * p.W + ((t - nPT) * kKeys >> 5)) : "memory");
     // ---- the query rows as fragments (rows are columns of the products), where all warps find them
@@ -373,7 +380,7 @@ __global__ void __launch_bounds__(RowsGeo<D, NT>::THREADS, RowsGeo<D, NT>::BLOCK
             for (int e = 0; e < 4; ++e) s[0][e] += s1[0][e];
         }
         // ---- in log2 units, hidden ones -inf
-        const int t = first + i * WARPS;
+        const int t = first + i * step;
         bool raise = false;
         if (t >= nPT) {
             const int key0 = (t - nPT) * kKeys;
