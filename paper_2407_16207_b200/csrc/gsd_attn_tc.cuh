@@ -872,6 +872,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             n_my = (int)blockIdx.x < wu.units ? 1 : 0;
         }
         if (PAGED) {
+            __syncwarp();        // (lane 0 has set the barriers up, and every lane's copies report to them)
             if (n_my > 0) {
                 const UnitInfo u = unit_base<PLAN>(p, order, unit_index(0), wu);
                 pre = max(0, min(ST, min(u.nPT - u.t_begin, u.ntiles)));
