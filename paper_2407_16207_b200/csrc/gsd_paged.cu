@@ -140,8 +140,9 @@ __global__ void __launch_bounds__(kThreads, kRotaryBlocks) paged_write_kernel(co
     if (begin < end && s_bad != 0x7FFFFFFF) flags |= GSD_DEV_BAD_PAGE;
     if (flags && a.status) atomicOr((unsigned*)a.status, flags);
     if (MODE != APPEND) {
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        // (not the aligned forms: the warps come here by way of branches that their threads took apart)
+        asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         if (blockIdx.x == 0 && tid == 0) {
             const int bad = s_bad;
             a.seq_lens[b] = bad == 0x7FFFFFFF ? L + n : max(L, min(L + n, bad << a.page_log2));
