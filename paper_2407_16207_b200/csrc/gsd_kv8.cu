@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) kv8_write_kernel(WriteArgs a) {
         s.L = s.L < 0 ? 0 : a.Lmax;
     }
     // (only now may another CTA of the cluster write the length)
-    if (CLUSTER) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (CLUSTER) asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     if (a.nodes) {
         // the valid node ids of the path, in order: a ballot a warp, a scan over the warps
         want = min(min(want, a.Tcap), GSD_MAX_NODES);
@@ -245,7 +245,8 @@ __global__ void __launch_bounds__(kThreads) kv8_write_kernel(WriteArgs a) {
     }
     if (flags && a.status) atomicOr((unsigned*)a.status, flags);
     if (CLUSTER) {
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        // (not the aligned form: the threads come from branches of their own)
+        asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
         if (blockIdx.x == 0 && tid == 0) a.seq_lens[b] = s.L + s.n;
     }
 }

@@ -26,7 +26,7 @@ def test_lanes_that_copy_wait_for_the_lane_that_sets_the_barriers_up(name, begin
     assert "__syncwarp();" in part
 
 
-@pytest.mark.parametrize("name", ["gsd_paged.cu", "gsd_attn_paged_rows.cu"])
+@pytest.mark.parametrize("name", ["gsd_paged.cu", "gsd_attn_paged_rows.cu", "gsd_kv8.cu"])
 def test_clusters_meet_without_the_aligned_forms(name):
     # those want a whole warp to come together, which nothing promises behind branches of single threads
     lines = [line for line in source(name).splitlines() if "barrier.cluster." in line]
