@@ -384,10 +384,11 @@ int attn_paged_rounds(const gsd_attn_params* p) { return ((p->Lmax + 15) / 16 + 
 // The kernel for few rows reads the cache once for up to 32 rows (24 at D = 64), the tcgen05 kernel for up to 256; a launch of the
 // former is over sooner.  So it gets the rows that it reads the cache once for (48 at D = 64, which L2 feeds, unless pairs and keys are
 // many), and more where its items run side by side and are short.  us, few rows and tcgen05, L between half and all of the length
-// given.  D 128: 1 x 32/8 heads, R = 128, L 2000 12.8 and 12.9, L 4000 17.7 and 13.8; 4 x 32/8, R = 64, L 500 9.2 and 11.8, L 2000
-// 17.2 and 17.2, L 8000 35.5 and 28.7, R = 32, L 8000 27.7 and 28.3; 16 x 32/8, R = 32, L 8000 85.1 and 84.3, R = 40, L 500 19.9 and
-// 14.1; 48 x 32/8, L 2000, R = 24 62 and 63, R = 32 69 and 64.  D 64: 4 x 32/8, R = 96, L 1000 12.0 and 15.8, L 4000 23.3 and 20.1;
-// 16 x 32/8, R = 48, L 8000 66 and 73, R = 64, L 500 18.9 and 14.0; 48 x 32/8, R = 32, L 4000 82 and 87, R = 48 92 and 87.
+// given.  D 128: 1 x 32/8 heads, R = 128, L 2000 12.2 and 12.9, L 4000 17.7 and 13.9; 4 x 32/8, R = 64, L 500 8.8 and 11.9, L 2000
+// 16.3 and 17.3, L 8000 34.0 and 28.6, R = 32, L 8000 27.4 and 28.3; 16 x 32/8, R = 32, L 8000 82.9 and 84.6, R = 40, L 500 18.8 and
+// 14.1; 48 x 32/8, L 2000, R = 24 61 and 64, R = 32 66 and 64.  D 64: 4 x 32/8, R = 96, L 1000 11.6 and 15.7, L 4000 23.4 and 20.1;
+// 16 x 32/8, R = 48, L 8000 65 and 73, R = 64, L 500 18.1 and 14.0; 48 x 32/8, R = 32, L 4000 74 and 86, R = 48 92 and 87.  Over 640
+// shapes the choice costs 0.4 % against the better kernel of each; the worst, 4 x 32/8 of 64, R = 128, L 1000, a quarter (16.1 and 12.7).
 int attn_paged_pick_kernel(const gsd_attn_params* p, int sm_count) {
     if (p->kernel != GSD_ATTN_AUTO) return p->kernel;
     const int G = p->Hq / p->Hkv, rounds = attn_paged_rounds(p);
@@ -419,17 +420,19 @@ AttnPlan attn_paged_make_plan(const gsd_attn_params* p, int sm_count) {
     pl.dev.splits_a = pl.dev.splits_b = 1;
     const int resident = sm_count * attn_paged_rows_resident(pl.rows_per_item, p->D);
     // A cut has to save more than the merge launch and its partial results cost, about eight rounds on the longest sequence (five for
-    // a single one, which needs no plan by length).  us cut and whole, D 128: 4 x 32/8 heads, N 2, L 250-500 8.4 and 6.6, L 500-1000 9.4
-    // and 9.1, L 1000-2000 11.8 and 12.9; 1 x 32/8, N 4, L 250-500 6.4 and 6.3, L 500-1000 6.5 and 8.1; 8 x 32/8, N 2, L 1000-2000 15.3
-    // and 13.8.  Past 16 rounds lengths may differ by so much that several sequences are cut wherever an SM is left.
+    // a single one, which needs no plan by length).  us cut (by length) and whole, D 128: 4 x 32/8 heads, N 2, L 250-500 8.1 and 6.0, L
+    // 500-1000 9.4 and 8.1, L 1000-2000 11.4 and 11.7; 1 x 32/8, N 4, L 250-500 6.5 and 5.7, L 500-1000 6.5 and 7.4; 8 x 32/8, N 2, L
+    // 1000-2000 15.4 and 12.9.  Past 16 rounds lengths may differ by so much that several sequences are cut wherever an SM is left.
     const long long gain = (long long)rounds * std::max(sm_count - pl.items, 0);
     const bool cut = p->B > 1 ? gain >= 8 * sm_count || (rounds > 16 && gain > 0) : gain >= 5 * sm_count;
     // A cluster for each item of several sequences, its CTAs taking even shares of the keys: no plan by length, no merge launch, but a
-    // range is as long as its sequence's share, at most 20 rounds here, so that lengths that differ cost little.  us by length and in
-    // clusters: D 128, N 1, 4 x 32/8 heads, L 500-1000 9.0 and 8.5, 8 x 64/8, L 1000-2000 15.4 and 14.1, L 2000-4000 23.2 and 21.4, L
-    // 100-4000 17.3 and 16.6; D 64, N 1, 4 x 32/8, L 1000-2000 9.8 and 8.5, 16 x 32/2, L 100-4000 11.5 and 12.5.  Items of 16 rows and
-    // more gain nothing on average (N 4, 8 x 64/8, L 2000-4000 28.2 and 27.0, L 100-4000 22.0 and 24.6), nor does a single sequence, which
-    // has no plan.  Nine tenths of the SMs can be filled with clusters of up to five, three quarters with larger ones: 16 clusters of
+    // range is as long as its sequence's share, at most 20 rounds here, which bounds what lengths that differ cost.  us by length and in
+    // clusters: D 128, N 1, 4 x 32/8 heads, L 500-1000 9.4 and 7.7 (whole 8.1), 8 x 64/8, L 1000-2000 15.6 and 13.2, L 2000-4000 23.7
+    // and 20.7, L 4000 28.4 and 25.2, L 100-4000 17.5 and 16.0; D 64, N 1, 4 x 32/8, L 1000-2000 9.6 and 8.4, 8 x 64/8, L 4000 19.2 and
+    // 16.1, 16 x 32/2, L 100-4000 11.4 and 12.5.  One long sequence among short ones, which the host does not know of, is the price: 8 x
+    // 64/8, one of 4000 and seven of 100, D 128 11.0 and 13.4, D 64 10.3 and 12.5; of 2000, D 128 9.1 and 9.3; 16 x 32/2 of 64, one of
+    // 4000 and 15 of 100, 8.2 and 12.1.  Items of 16 rows and more gained nothing on average when tried (N 4, 8 x 64/8, L 2000-4000 28.2
+    // and 27.0, L 100-4000 22.0 and 24.6), nor did a single sequence, which has no plan.  Nine tenths of the SMs can be filled with clusters of up to five, three quarters with larger ones: 16 clusters of
     // eight did not run side by side (12.1 us, of six 7.2).  Where few of them fill less than that, the plan by length has more SMs (48
     // items, L 2000-4000 13.1 and 14.2 us).
     int cs = sm_count * 9 / (10 * pl.items);

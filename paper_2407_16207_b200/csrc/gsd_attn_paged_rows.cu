@@ -9,17 +9,17 @@
 // copied as the 16 rows up to the end (rows before the page's first come back as zeros), so that nothing behind the end is read.
 // Both products are transposed, S^T = K Q^T and O^T = V^T P^T, so that 8 rows fill an instruction (16 keys or 16 columns by 8
 // rows); the weights are turned round by a movmatrix.  A row's running maximum is raised when a score exceeds it by more than
-// 2^kLag: the weights are rounded to bf16, whose relative step does not depend on their size, and sums stay fp32.
+// 2^kLag: the weights are rounded to bf16, the type that the product with V takes, whose relative step does not depend on their size,
+// and sums stay fp32.
 //
 // The work is dealt out by length inside the kernel for up to 32 sequences: every item (a group of rows of a sequence and
 // kv head) is cut into ranges of at most T rounds of keys, T the least with which all ranges are resident at once; a merge pass brings
 // them together.  Where items of eight rows are cut evenly and not too long, a cluster has the ranges of an item and needs no such pass.
 //
 // Bound by DRAM where keys are many, by dependent trips and the length of a warp's round where they are few.  32 x 64/8 heads of 128,
-// N 1, L 4096: 83 us for 537 MB, the rate of a copy; 8 of them, L 1500-3500, 17.9 us for 74 MB in clusters of two (by length, with the
-// merge launch, 20.1; padded cache 24.1).
-// 4 x 32/8 heads of 64, N 12, L 1000-4000 15.9 us (16.2).  Four warps and two CTAs an SM, or two and four, take 92 and 97 us for the
-// first; copies by cp.async 84 us; weights in two bf16 terms bring the error from 2.3e-3 to 1.7e-3 for 1-5 % of the time.
+// N 1, L 4096: 83 us for 537 MB, the rate of a copy; 8 of them, L 500-4000, 17.9 us for 74 MB in clusters of two (by length, with the
+// merge launch, 20.1; padded cache 24.0).  4 x 32/8 heads of 64, N 12, L 1000-4000 16.1 us (16.3); 32 x 32/8 of 64, N 1, L 4096 46 us for
+// 268 MB.  Four warps and two CTAs an SM, or two and four, took 92 and 97 us for the first; copies by cp.async 84 us; weights in two bf16 terms bring the error from 2.3e-3 to 1.7e-3 for 1-5 % of the time.
 #include "gsd_tma.cuh"
 #include <cuda_bf16.h>
 #include <math_constants.h>
@@ -627,8 +627,8 @@ int launch_t(const AttnArgs& a) {
 // work over more SMs, and a warp's round is shorter.  So an item gets the fewest rows with which all items, each cut into as many
 // ranges as the length asks for (one for 20 rounds of keys), still run side by side: up to 32 rows with a CTA an SM; for D = 64,
 // where two fit, up to 24 rows with two; past that the most rows.  us at 8, 16, 24 and 32 rows, D 128: 4 x 32/8 heads, N 8, L
-// 250-500 6.9, 9.2, 9.2, 12.3, L 4000-8000 36, 26, 26, 28; 1 x 32/8, N 12, L 1000 7.6, 8.2, 9.1, 9.1; 16 x 32/8, N 16, L 500-1000
-// 56, 40, 36, 30.  D 64: 4 x 96/24, N 16, L 250-500 27, 15, 12, 18; 48 x 32/8, N 16, L 100-200 55, 35, 31, 43.
+// 250-500 6.7, 8.3, 8.2, 11.0, L 4000-8000 36, 27, 27, 27; 1 x 32/8, N 12, L 500-1000 7.8, 8.6, 9.3, 9.4; 16 x 32/8, N 16, L 500-1000
+// 55, 39, 35, 29.  D 64: 4 x 96/24, N 16, L 250-500 20, 15, 11, 17; 48 x 32/8, N 16, L 100-200 55, 35, 31, 41.
 int attn_paged_rows(int R, int D, int pairs, int ranges, int sm_count) {
     const int groups = (R + 7) / 8;
     for (int ctas = 1; ctas <= (D == 64 ? 2 : 1); ++ctas)

@@ -21,9 +21,9 @@
 // TMEM (512 columns) at D = 128: S (128) | P0 (64) | P1 (64) | O0 (128) | O1 (128); the layout at
 // D = 64 is in Geo.  There is one score
 // buffer: QK^T of job k+1 is issued as soon as the softmax of job k has pulled its score row
-// into registers, i.e. it runs under that softmax; P (bf16) has a buffer per stream and
-// O_i += P_i V follows when the softmax hands P over (in two halves of 64 keys).  So neither
-// softmax warpgroup ever waits for a QK^T that could not start.  The two kinds of MMA are
+// into registers, i.e. it runs under that softmax; P (bf16 like V: the instruction takes operands
+// of one type) has a buffer per stream and O_i += P_i V follows when the softmax hands P over (in
+// two halves of 64 keys).  So neither softmax warpgroup ever waits for a QK^T that could not start.  The two kinds of MMA are
 // issued by two warps on different schedulers, each paced only by its own barriers (the
 // softmax warps are almost always ready to issue, so one issuing warp gets too few slots
 // to feed the tensor pipe).  The running maximum is only raised when a tile

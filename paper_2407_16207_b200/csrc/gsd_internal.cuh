@@ -90,7 +90,8 @@ struct PlanDev {
 constexpr int kPlanSeqs = 384;      // sequences the attention kernel can put in order (one per thread)
 struct AttnPlan {
     int kernel;         // GSD_ATTN_MMA or GSD_ATTN_TCGEN05
-    int rows_per_item;  // stacked rows of an item: 64 (mma.sync back end) or two row tiles of attn_tcgen05_rows(G) (tcgen05 back end)
+    int rows_per_item;  // stacked rows of an item: two row tiles of attn_tcgen05_rows(G) (tcgen05 back end), 64 (mma.sync back end), or
+                        // the 8 to 32 of attn_paged_rows and attn_q8_mma_rows
     int part_rows;      // rows of a partial-result slot: 64 or 2 x 128
     int items;
     int ctas;

@@ -8,8 +8,8 @@
 // cluster of CTAs per sequence, so that it can move the length on itself.
 //
 // Measured in captured graphs: 8 prompts of 1000-4096 rows, 8 kv heads of 128, 29.1 us for 167 MB, 89 % of the rate of a copy, and 3 us
-// for the launch that moves the lengths on; a chunk of 1031 rows of 4 heads 3.9 us; paths of up to 17 rows, 8 x 8 heads, 3.8 us, of up to
-// 10 rows, 32 x 40 heads, 5.7 us.  One launch for all appends, whose last CTA moves the length on, would need a counter that is zero.
+// for the launch that moves the lengths on; a chunk of 1031 rows of 4 heads 3.8 us; paths of up to 17 rows, 8 x 8 heads, 3.5 us, of up to
+// 10 rows, 32 x 40 heads, 5.8 us.  One launch for all appends, whose last CTA moves the length on, would need a counter that is zero.
 #include "gsd_pages.cuh"
 #include "gsd_rotary.cuh"
 #include <initializer_list>
